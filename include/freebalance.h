@@ -411,6 +411,77 @@ fb_status fb_apply_swaps_staged(fb_ctx* ctx, void* slot_weights, uint64_t expert
                                 const fb_swap* swaps, const int32_t* n_swaps, int32_t max_swaps,
                                 uint64_t staging_bytes, fb_stream plan_stream, fb_stream copy_stream);
 
+/* ---- the experts behind the dispatch index (Preliminary: a layer's output is the sum of w_e times expert e of the
+ * token, over the token's top k) ----
+ * What follows fb_route_dispatch / fb_layer_step on the GPU that holds the weights.  An expert is three matrices: gate
+ * and up projection [inter][d] each, and down projection [d][inter].  In dispatch order (position p of perm):
+ *   h[p] = silu(x[t] gate^T) * (x[t] up^T)   t = perm[p] / k     fb_expert_matmul, FB_ACT_SWIGLU, with perm
+ *   y[p] = h[p] down^T                                           fb_expert_matmul, FB_ACT_NONE, without perm
+ *   out[t] = sum over j of topk_w[t][j] * y[inv_perm[t k + j]]   fb_combine
+ * Weights are bf16, or e4m3 with a scale for each block of 128 x 128; the rows that meet e4m3 weights are e4m3 with a
+ * scale for each 128 columns (fb_quantize_rows; the SwiGLU product can hand out such rows itself).  Forward only: router
+ * and experts are frozen here.  A row's
+ * result does not depend on the rows beside it, and equal calls give equal bits.
+ * All three run on ctx's device, allocate nothing, use no scratch of the context (calls may overlap on any streams) and
+ * may be captured.  Sums, norms and scales are formed in 32 bits. */
+
+typedef enum {
+  FB_ACT_NONE = 0,
+  FB_ACT_SWIGLU = 1                        /* rows [0, n / 2) of a slot's matrix are gate, the others up */
+} fb_act;
+
+#define FB_DTYPE_E4M3 2                    /* (FB_DTYPE_BF16 and FB_DTYPE_F32: below) */
+
+/* One matrix [n][K] (K contiguous) per slot.  slot_bytes: from one slot's matrix to the next, so the matrices may be
+ * parts of the slot images that fb_apply_swaps exchanges; a multiple of 16, below 2^40.
+ * Limits: 1 <= n_slots <= 256; K a multiple of 8 (bf16) or 16 (e4m3); n a multiple of 8, with FB_ACT_SWIGLU of 32.
+ * scale (e4m3 only): dev f32 [row blocks][ceil(K / 128)] per slot, slot s at scale + s * scale_slot; the values are
+ * w * scale.  Row blocks: ceil(n / 128), with FB_ACT_SWIGLU ceil(n / 256) of gate, then as many of up. */
+typedef struct {
+  int32_t dtype;             /* FB_DTYPE_BF16 or FB_DTYPE_E4M3                                  */
+  int32_t act;               /* fb_act                                                          */
+  int32_t n_slots, n, K;
+  const void* w;             /* dev, 16-byte aligned                                            */
+  uint64_t slot_bytes;
+  const float* scale;        /* dev f32 or NULL (bf16)                                          */
+  uint64_t scale_slot;       /* floats                                                          */
+} fb_expert_matrix;
+
+/* Rows to e4m3 with block scales, for every block of 128 columns (the last one of a row may be shorter):
+ * a = max(max |x|, 2^-100), scale = a / 448, q = x * (448 / a) rounded to nearest even.  A NaN stays in its place; a
+ * block that holds an infinity becomes NaN and zeros under an infinite scale.
+ *   x      dev bf16 [rows][n], n a multiple of 16
+ *   q      dev e4m3 [rows][n]                out
+ *   scale  dev f32 [rows][ceil(n / 128)]     out */
+fb_status fb_quantize_rows(fb_ctx* ctx, const void* x, int64_t rows, int32_t n, void* q, float* scale, fb_stream stream);
+
+/* Product grouped by slot: for the positions slot_offsets[s] <= p < slot_offsets[s + 1]
+ *   out[p - slot_offsets[0]] = act(x[r] W_s^T),  r = perm[p] / k (k of ctx)  or, without perm, p - slot_offsets[0].
+ *   x             dev [x_rows][K] of the matrix's type
+ *   x_scale       dev f32 [x_rows][ceil(K / 128)] (e4m3), else NULL
+ *   slot_offsets  dev u32 [n_slots + 1] as written by fb_route_dispatch; a rank that holds the slots from s0 on passes
+ *                 slot_offsets + s0 and its own matrices.  NULL: one slot (n_slots 1) that has all rows
+ *   perm          dev i32, indexed by p, or NULL
+ *   rows          rows that out holds; slot_offsets[n_slots] - slot_offsets[0] may be less, and rows of out behind it
+ *                 are left as they are.  Slots may be empty.
+ *   out           dev bf16 [rows][n_out], n_out = n (n / 2 with FB_ACT_SWIGLU), rounded once from 32 bits; with out_scale
+ *                 (e4m3 and FB_ACT_SWIGLU only) e4m3 [rows][n_out], quantised as by fb_quantize_rows from the 32-bit values
+ *   out_scale     dev f32 [rows][ceil(n_out / 128)] or NULL
+ * out overlaps no input.  One launch.  Device status FB_ERR_RANGE: offsets that do not rise or pass `rows` (that
+ * slot's rows are left out), an entry of perm outside x (row 0 is read instead). */
+fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* matrix, const void* x, const float* x_scale, int32_t x_rows,
+                           const uint32_t* slot_offsets, const int32_t* perm, int32_t rows, void* out, float* out_scale,
+                           fb_stream stream);
+
+/* out[t] = sum over j of w[t][j] * rows[inv_perm[t k + j]] (+ addend[t]), j ascending, in 32 bits, rounded once.
+ *   rows      dev bf16 [T k][n] (k of ctx), n a multiple of 8
+ *   w         dev f32 [T][k], inv_perm dev i32 [T k]: as written by fb_route_dispatch
+ *   addend    dev bf16 [T][n] or NULL (a shared expert's output, a residual); may be out itself
+ *   out       dev bf16 [T][n]
+ * Device status FB_ERR_RANGE: an entry of inv_perm outside [0, T k) (row 0 is read instead). */
+fb_status fb_combine(fb_ctx* ctx, const void* rows, const float* w, const int32_t* inv_perm, int32_t T, int32_t n,
+                     const void* addend, void* out, fb_stream stream);
+
 /* ---- prediction-quality metrics (Evaluation, "Metrics"); not part of the per-layer hot path ----
  * These three take no context and launch on the CURRENT device, which must be the one `stream` and the buffers
  * belong to. */

@@ -39,6 +39,12 @@ class FbBudget(ctypes.Structure):
                 ("mode", ctypes.c_int32), ("frontier_width", ctypes.c_int32)]
 
 
+class FbExpertMatrix(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("n_slots", ctypes.c_int32), ("n", ctypes.c_int32),
+                ("K", ctypes.c_int32), ("w", ctypes.c_void_p), ("slot_bytes", ctypes.c_uint64),
+                ("scale", ctypes.c_void_p), ("scale_slot", ctypes.c_uint64)]
+
+
 FB_PLAN_LOOP, FB_PLAN_SWEEP, FB_PLAN_WIDE = 0, 1, 2
 
 
@@ -61,7 +67,7 @@ EXPORTS = ["fb_create", "fb_destroy", "fb_budget_ns", "fb_swap_cost_ns", "fb_pre
            "fb_attention_set_time_ns", "fb_attention_reset", "fb_dispatch_slot_counts", "fb_dispatch_globalize",
            "fb_standin_attention", "fb_set_split", "fb_prediction_quality",
            "fb_layer_step_observed", "fb_staged_row_layout",
-           "fb_selftest_wait_progress", "fb_fail_launch"]
+           "fb_selftest_wait_progress", "fb_fail_launch", "fb_quantize_rows", "fb_expert_matmul", "fb_combine"]
 
 _lib = None
 
@@ -156,6 +162,12 @@ def lib() -> ctypes.CDLL:
     L.fb_calibrate_exchange.argtypes = [vp, u64, u64, i32] + [ctypes.POINTER(u64)] * 4 + [vp]
     L.fb_calibrate_exchange.restype = ctypes.c_int
     L.fb_topk_hits.restype = ctypes.c_int
+    L.fb_quantize_rows.argtypes = [vp, vp, ctypes.c_int64, i32, vp, vp, vp]
+    L.fb_quantize_rows.restype = ctypes.c_int
+    L.fb_expert_matmul.argtypes = [vp, ctypes.POINTER(FbExpertMatrix), vp, vp, i32, vp, vp, i32, vp, vp, vp]
+    L.fb_expert_matmul.restype = ctypes.c_int
+    L.fb_combine.argtypes = [vp, vp, vp, vp, i32, i32, vp, vp, vp]
+    L.fb_combine.restype = ctypes.c_int
     L.fb_router_floor.argtypes = [vp, ctypes.POINTER(FbRouter), vp, i32, i32, vp]
     L.fb_router_floor.restype = ctypes.c_int
     L.fb_time_next_router_launch.argtypes = [vp, vp, vp]
@@ -225,7 +237,26 @@ def fb_swap_cost_ns(budget: FbBudget, rank_a: int, rank_b: int) -> int:
     return int(lib().fb_swap_cost_ns(ctypes.byref(budget), rank_a, rank_b))
 
 
-FB_DTYPE_BF16, FB_DTYPE_F32 = 0, 1
+FB_DTYPE_BF16, FB_DTYPE_F32, FB_DTYPE_E4M3 = 0, 1, 2
+FB_ACT_NONE, FB_ACT_SWIGLU = 0, 1
+
+
+def make_expert_matrix(w: torch.Tensor, scale: Optional[torch.Tensor] = None, act: int = FB_ACT_NONE) -> FbExpertMatrix:
+    """w: [slots, n, K] bf16 or e4m3, each slot's matrix contiguous (slots may lie further apart: parts of slot images);
+    scale (e4m3): float32 [slots, row blocks, ceil(K / 128)], contiguous per slot."""
+    assert w.dim() == 3 and w.stride(2) == 1 and w.stride(1) == w.shape[2], "a slot's matrix must be contiguous"
+    assert w.dtype in (torch.bfloat16, torch.float8_e4m3fn)
+    e4m3 = w.dtype == torch.float8_e4m3fn
+    m = FbExpertMatrix(FB_DTYPE_E4M3 if e4m3 else FB_DTYPE_BF16, act, w.shape[0], w.shape[1], w.shape[2], w.data_ptr(),
+                       w.stride(0) * w.element_size(), None, 0)
+    if scale is not None:
+        rows = w.shape[1]
+        blocks = 2 * -(-(rows // 2) // 128) if act == FB_ACT_SWIGLU else -(-rows // 128)
+        assert scale.dtype == torch.float32 and scale.shape == (w.shape[0], blocks, -(-w.shape[2] // 128)), "one scale per block"
+        assert scale.stride(2) == 1 and scale.stride(1) == scale.shape[2], "a slot's scales must be contiguous"
+        m.scale, m.scale_slot = scale.data_ptr(), scale.stride(0)
+    m._keepalive = (w, scale)
+    return m
 
 
 def fb_row_cosine_mean(a: torch.Tensor, b: torch.Tensor, row_scratch: torch.Tensor, mean_out: torch.Tensor,
@@ -369,6 +400,20 @@ class Context:
         _check(lib().fb_layer_step_host(self._h, ctypes.byref(router), _ptr(h_prev_host), _ptr(H_host), T,
                                         _ptr(expert_to_slot_host), ctypes.byref(budget), layer_id,
                                         *[_ptr(o) for o in outs], _stream(stream)), "fb_layer_step_host")
+
+    def fb_quantize_rows(self, x, rows, n, q, scale, stream=None):
+        assert x.dtype == torch.bfloat16 and scale.dtype == torch.float32
+        _check(lib().fb_quantize_rows(self._h, _ptr(x), rows, n, _ptr(q), _ptr(scale), _stream(stream)), "fb_quantize_rows")
+
+    def fb_expert_matmul(self, matrix, x, x_scale, slot_offsets, perm, rows, out, out_scale=None, stream=None):
+        """x: [x_rows, K] of the matrix's type; out: [rows, n_out] bf16, or e4m3 with out_scale."""
+        assert x.dim() == 2 and x.shape[1] == matrix.K
+        _check(lib().fb_expert_matmul(self._h, ctypes.byref(matrix), _ptr(x), _ptr(x_scale), x.shape[0], _ptr(slot_offsets),
+                                      _ptr(perm), rows, _ptr(out), _ptr(out_scale), _stream(stream)), "fb_expert_matmul")
+
+    def fb_combine(self, rows, w, inv_perm, T, n, addend, out, stream=None):
+        _check(lib().fb_combine(self._h, _ptr(rows), _ptr(w), _ptr(inv_perm), T, n, _ptr(addend), _ptr(out), _stream(stream)),
+               "fb_combine")
 
     def fb_device_status(self, stream=None) -> int:
         word = ctypes.c_int32(0)

@@ -12,6 +12,7 @@
 #include "../../include/freebalance.h"
 #include "../../include/freebalance_aids.h"
 #include "fb_dispatch.cuh"
+#include "fb_experts.cuh"
 #include "fb_migrate.cuh"
 #include "fb_planner.cuh"
 #include "fb_quality.cuh"
@@ -508,9 +509,27 @@ int device_of(const void* p) {
   return (pa.type == cudaMemoryTypeDevice || pa.type == cudaMemoryTypeManaged) ? pa.device : -1;
 }
 
+// Kernel instances of the expert products: bf16, e4m3, e4m3 with rows that come out quantised (SwiGLU only).
+using ExpertKernelFn = void (*)(CUtensorMap, CUtensorMap, fb::ExpertParams);
+struct ExpertKernel {
+  ExpertKernelFn fn;
+  size_t smem;
+};
+template <bool kE4m3, bool kSwiglu, bool kQuantize>
+ExpertKernel expert_kernel_of() {
+  return {fb::fb_expert_matmul_kernel<kE4m3, kSwiglu, kQuantize>, fb::ExpertLayout<kE4m3, kSwiglu, kQuantize>::kDynamic};
+}
+ExpertKernel expert_kernel(bool e4m3, bool swiglu, bool quantize) {
+  if (!e4m3) return swiglu ? expert_kernel_of<false, true, false>() : expert_kernel_of<false, false, false>();
+  if (!swiglu) return expert_kernel_of<true, false, false>();
+  return quantize ? expert_kernel_of<true, true, true>() : expert_kernel_of<true, true, false>();
+}
+
 // A fixed one-swap plan over two slots for fb_calibrate_exchange: [placement: 2][swap: 4][n: 1].
 // Constant data inside the library image, so the calibration allocates nothing.
 __device__ const int32_t g_calibration_plan[8] = {0, 1, 0, 1, 0, 1, 1, 0};
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 template <typename Tp>
 bool dev_alloc(Tp** p, size_t count) {
@@ -639,6 +658,7 @@ static fb_status set_up_device(fb_ctx* ctx, int device, const DeviceLimits& dev)
   const int plan_general = raise(reinterpret_cast<const void*>(fb::fb_plan_kernel<true>));
   const int plan_uniform = raise(reinterpret_cast<const void*>(fb::fb_plan_kernel<false>));
   ctx->own_sm.smem = plan_general < plan_uniform ? plan_general : plan_uniform;
+  for (int i = 0; i < 5; ++i) raise(reinterpret_cast<const void*>(expert_kernel(i >= 2, i == 1 || i >= 3, i == 4).fn));
   int least = 0;
   ok = ok && cudaDeviceGetStreamPriorityRange(&least, &ctx->own_sm.priority) == cudaSuccess;
   if (!ok) { cudaGetLastError(); return FB_ERR_CUDA; }
@@ -1120,6 +1140,130 @@ fb_status fb_apply_swaps_staged(fb_ctx* ctx, void* slot_weights, uint64_t expert
     }
   }
   return ok ? FB_OK : FB_ERR_CUDA;
+}
+
+fb_status fb_quantize_rows(fb_ctx* ctx, const void* x, int64_t rows, int32_t n, void* q, float* scale, fb_stream stream_) {
+  if (!ctx || rows < 0 || n <= 0 || n % 16 != 0) return FB_ERR_INVALID_ARG;
+  if (rows == 0) return FB_OK;
+  if (!x || !q || !scale || !aligned16(x) || !aligned16(q)) return FB_ERR_INVALID_ARG;
+  const int blocks_k = (n + 127) / 128;
+  const int64_t per_block = fb::kQuantizeThreads / 16 * fb::kQuantizeUnroll;
+  if (rows > (int64_t{1} << 31) * per_block / blocks_k - per_block) return FB_ERR_UNSUPPORTED_SHAPE;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return FB_ERR_CUDA;
+  const int64_t blocks = (rows * blocks_k + per_block - 1) / per_block;
+  return launch_counted(ctx, fb::fb_quantize_rows_kernel, static_cast<int>(blocks), fb::kQuantizeThreads, kAnyShare,
+                        static_cast<cudaStream_t>(stream_), static_cast<const __nv_bfloat16*>(x), static_cast<long long>(rows), n,
+                        blocks_k, static_cast<uint8_t*>(q), scale) == cudaSuccess ? FB_OK : FB_ERR_CUDA;
+}
+
+fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x, const float* x_scale, int32_t x_rows,
+                           const uint32_t* slot_offsets, const int32_t* perm, int32_t rows, void* out, float* out_scale,
+                           fb_stream stream_) {
+  if (!ctx || !m || x_rows < 0 || rows < 0) return FB_ERR_INVALID_ARG;
+  if (m->dtype != FB_DTYPE_BF16 && m->dtype != FB_DTYPE_E4M3) return FB_ERR_INVALID_ARG;
+  if (m->act != FB_ACT_NONE && m->act != FB_ACT_SWIGLU) return FB_ERR_INVALID_ARG;
+  const bool e4m3 = m->dtype == FB_DTYPE_E4M3, swiglu = m->act == FB_ACT_SWIGLU;
+  if (m->n_slots <= 0 || m->n <= 0 || m->K <= 0 || !m->w || !aligned16(m->w) || m->slot_bytes % 16 != 0) return FB_ERR_INVALID_ARG;
+  if (m->n_slots > FB_MAX_EXPERTS || m->K % (e4m3 ? 16 : 8) != 0 || m->n % (swiglu ? 32 : 8) != 0) return FB_ERR_UNSUPPORTED_SHAPE;
+  const uint64_t row_bytes = static_cast<uint64_t>(m->K) * (e4m3 ? 1 : 2);
+  if (m->slot_bytes >= (uint64_t{1} << 40) || row_bytes * static_cast<uint64_t>(m->n) >= (uint64_t{1} << 40)) return FB_ERR_UNSUPPORTED_SHAPE;
+  if (m->n_slots > 1 && m->slot_bytes < row_bytes * static_cast<uint64_t>(m->n)) return FB_ERR_INVALID_ARG;
+  if (slot_offsets == nullptr && (m->n_slots != 1 || perm != nullptr)) return FB_ERR_INVALID_ARG;
+  if (e4m3 != (m->scale != nullptr) || (out_scale != nullptr && !(e4m3 && swiglu))) return FB_ERR_INVALID_ARG;
+  if (perm == nullptr && x_rows < rows) return FB_ERR_INVALID_ARG;
+  if (rows == 0) return FB_OK;
+  if (x_rows == 0 || !x || !out || !aligned16(x) || !aligned16(out) || e4m3 != (x_scale != nullptr)) return FB_ERR_INVALID_ARG;
+  fb::ExpertParams p;
+  memset(&p, 0, sizeof(p));
+  p.slot_offsets = slot_offsets;
+  p.perm = perm;
+  p.x_scale = x_scale;
+  p.w_scale = m->scale;
+  p.w_scale_slot = m->scale_slot;
+  p.out = out;
+  p.out_scale = out_scale;
+  p.status = ctx->status;
+  p.n_slots = m->n_slots;
+  p.k = ctx->cfg.k;
+  p.x_rows = x_rows;
+  p.rows = rows;
+  const int step = e4m3 ? 128 : 64;
+  p.num_kb = (m->K + step - 1) / step;
+  p.n_out = swiglu ? m->n / 2 : m->n;
+  p.m_blocks = (m->n + fb::kExpertTileM - 1) / fb::kExpertTileM;
+  p.scale_k = (m->K + 127) / 128;
+  // a slot of c rows has at most ceil(c / 256) tiles of rows
+  const int64_t tiles = (rows / fb::kExpertTileN + (m->n_slots < rows ? m->n_slots : rows)) * static_cast<int64_t>(p.m_blocks);
+  if (tiles >= (int64_t{1} << 31)) return FB_ERR_UNSUPPORTED_SHAPE;
+  CUtensorMap map_x, map_w;
+  const CUtensorMapDataType type = e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  auto encode = [&](CUtensorMap* map, int dims, const void* ptr, const cuuint64_t* size, const cuuint64_t* stride, const cuuint32_t* box) {
+    const cuuint32_t one[5] = {1, 1, 1, 1, 1};
+    return ctx->encode(map, type, static_cast<cuuint32_t>(dims), const_cast<void*>(ptr), size, stride, box, one,
+                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  const cuuint64_t K = static_cast<cuuint64_t>(m->K), E = static_cast<cuuint64_t>(m->n_slots);
+  const cuuint32_t width = static_cast<cuuint32_t>(step);
+  // one slot has no stride: any value that the map takes
+  const cuuint64_t slot_bytes = m->n_slots > 1 ? m->slot_bytes : (row_bytes * static_cast<uint64_t>(m->n) + 15) / 16 * 16;
+  bool ok;
+  {
+    const cuuint64_t size[2] = {K, static_cast<cuuint64_t>(x_rows)}, stride[1] = {row_bytes};
+    const cuuint32_t box[2] = {width, 1};                          // gathered row by row
+    ok = encode(&map_x, 2, x, size, stride, box);
+  }
+  if (swiglu) {                                                    // 16 rows of gate, 16 of up, ..
+    const cuuint64_t size[5] = {K, 16, 2, static_cast<cuuint64_t>(p.n_out / 16), E};
+    const cuuint64_t stride[4] = {row_bytes, row_bytes * p.n_out, row_bytes * 16, slot_bytes};
+    const cuuint32_t box[5] = {width, 16, 2, 4, 1};
+    ok = ok && encode(&map_w, 5, m->w, size, stride, box);
+  } else {
+    const cuuint64_t size[3] = {K, static_cast<cuuint64_t>(m->n), E}, stride[2] = {row_bytes, slot_bytes};
+    const cuuint32_t box[3] = {width, 128, 1};
+    ok = ok && encode(&map_w, 3, m->w, size, stride, box);
+  }
+  if (!ok) return FB_ERR_CUDA;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return FB_ERR_CUDA;
+  const ExpertKernel kernel = expert_kernel(e4m3, swiglu, out_scale != nullptr);
+  const int64_t pairs = tiles < ctx->max_clusters[1] ? tiles : ctx->max_clusters[1];
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs), 1, 1);
+  cfg.blockDim = dim3(fb::kExpertThreads, 1, 1);
+  cfg.dynamicSmemBytes = kernel.smem;
+  cfg.stream = static_cast<cudaStream_t>(stream_);
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  const cudaError_t err = launch_refused(ctx) ? cudaErrorUnknown : cudaLaunchKernelEx(&cfg, kernel.fn, map_x, map_w, p);
+  return err == cudaSuccess ? FB_OK : FB_ERR_CUDA;
+}
+
+fb_status fb_combine(fb_ctx* ctx, const void* rows, const float* w, const int32_t* inv_perm, int32_t T, int32_t n, const void* addend,
+                     void* out, fb_stream stream_) {
+  if (!ctx || T < 0 || n <= 0 || n % 8 != 0) return FB_ERR_INVALID_ARG;
+  if (T == 0) return FB_OK;
+  if (!rows || !w || !inv_perm || !out || !aligned16(rows) || !aligned16(out) || !aligned16(addend)) return FB_ERR_INVALID_ARG;
+  const int k = ctx->cfg.k, pieces = (n / 8 + fb::kCombineThreads - 1) / fb::kCombineThreads;
+  if (static_cast<int64_t>(T) * (pieces > k ? pieces : k) >= (int64_t{1} << 31)) return FB_ERR_UNSUPPORTED_SHAPE;
+  using CombineFn = void (*)(const __nv_bfloat16*, const float*, const int32_t*, int, int, int, const __nv_bfloat16*, __nv_bfloat16*, int32_t*);
+  static constexpr CombineFn kKernels[FB_MAX_TOPK] = {fb::fb_combine_kernel<1>, fb::fb_combine_kernel<2>, fb::fb_combine_kernel<3>,
+                                                      fb::fb_combine_kernel<4>, fb::fb_combine_kernel<5>, fb::fb_combine_kernel<6>,
+                                                      fb::fb_combine_kernel<7>, fb::fb_combine_kernel<8>};
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return FB_ERR_CUDA;
+  return launch_counted(ctx, kKernels[k - 1], T * pieces, fb::kCombineThreads, kAnyShare, static_cast<cudaStream_t>(stream_),
+                        static_cast<const __nv_bfloat16*>(rows), w, inv_perm, T, n, pieces, static_cast<const __nv_bfloat16*>(addend),
+                        static_cast<__nv_bfloat16*>(out), ctx->status) == cudaSuccess ? FB_OK : FB_ERR_CUDA;
 }
 
 fb_status fb_row_cosine_mean(const void* a, const void* b, int64_t rows, int32_t n, int32_t dtype,
