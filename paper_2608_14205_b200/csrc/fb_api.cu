@@ -13,6 +13,7 @@
 #include "../../include/freebalance_aids.h"
 #include "fb_dispatch.cuh"
 #include "fb_experts.cuh"
+#include "fb_experts_e4m3.cuh"
 #include "fb_migrate.cuh"
 #include "fb_planner.cuh"
 #include "fb_quality.cuh"
@@ -515,14 +516,14 @@ struct ExpertKernel {
   ExpertKernelFn fn;
   size_t smem;
 };
-template <bool kE4m3, bool kSwiglu, bool kQuantize>
-ExpertKernel expert_kernel_of() {
-  return {fb::fb_expert_matmul_kernel<kE4m3, kSwiglu, kQuantize>, fb::ExpertLayout<kE4m3, kSwiglu, kQuantize>::kDynamic};
-}
 ExpertKernel expert_kernel(bool e4m3, bool swiglu, bool quantize) {
-  if (!e4m3) return swiglu ? expert_kernel_of<false, true, false>() : expert_kernel_of<false, false, false>();
-  if (!swiglu) return expert_kernel_of<true, false, false>();
-  return quantize ? expert_kernel_of<true, true, true>() : expert_kernel_of<true, true, false>();
+  if (!e4m3) {
+    if (swiglu) return {fb::fb_expert_matmul_kernel<true>, fb::ExpertLayout<true>::kDynamic};
+    return {fb::fb_expert_matmul_kernel<false>, fb::ExpertLayout<false>::kDynamic};
+  }
+  if (!swiglu) return {fb::fb_expert_matmul_e4m3_kernel<false, false>, fb::kE4m3Dynamic};
+  if (!quantize) return {fb::fb_expert_matmul_e4m3_kernel<true, false>, fb::kE4m3Dynamic};
+  return {fb::fb_expert_matmul_e4m3_kernel<true, true>, fb::kE4m3Dynamic};
 }
 
 // A fixed one-swap plan over two slots for fb_calibrate_exchange: [placement: 2][swap: 4][n: 1].
@@ -1167,7 +1168,7 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   if (m->n_slots <= 0 || m->n <= 0 || m->K <= 0 || !m->w || !aligned16(m->w) || m->slot_bytes % 16 != 0) return FB_ERR_INVALID_ARG;
   if (m->n_slots > FB_MAX_EXPERTS || m->K % (e4m3 ? 16 : 8) != 0 || m->n % (swiglu ? 32 : 8) != 0) return FB_ERR_UNSUPPORTED_SHAPE;
   const uint64_t row_bytes = static_cast<uint64_t>(m->K) * (e4m3 ? 1 : 2);
-  if (m->slot_bytes >= (uint64_t{1} << 40) || row_bytes * static_cast<uint64_t>(m->n) >= (uint64_t{1} << 40)) return FB_ERR_UNSUPPORTED_SHAPE;
+  if (row_bytes >= (uint64_t{1} << 31) || m->slot_bytes >= (uint64_t{1} << 40) || row_bytes * static_cast<uint64_t>(m->n) >= (uint64_t{1} << 40)) return FB_ERR_UNSUPPORTED_SHAPE;
   if (m->n_slots > 1 && m->slot_bytes < row_bytes * static_cast<uint64_t>(m->n)) return FB_ERR_INVALID_ARG;
   if (slot_offsets == nullptr && (m->n_slots != 1 || perm != nullptr)) return FB_ERR_INVALID_ARG;
   if (e4m3 != (m->scale != nullptr) || (out_scale != nullptr && !(e4m3 && swiglu))) return FB_ERR_INVALID_ARG;
@@ -1178,6 +1179,7 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   memset(&p, 0, sizeof(p));
   p.slot_offsets = slot_offsets;
   p.perm = perm;
+  p.x = x;
   p.x_scale = x_scale;
   p.w_scale = m->scale;
   p.w_scale_slot = m->scale_slot;
@@ -1188,13 +1190,14 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   p.k = ctx->cfg.k;
   p.x_rows = x_rows;
   p.rows = rows;
+  p.row_bytes = static_cast<int32_t>(row_bytes);
   const int step = e4m3 ? 128 : 64;
   p.num_kb = (m->K + step - 1) / step;
   p.n_out = swiglu ? m->n / 2 : m->n;
   p.m_blocks = (m->n + fb::kExpertTileM - 1) / fb::kExpertTileM;
   p.scale_k = (m->K + 127) / 128;
-  // a slot of c rows has at most ceil(c / 256) tiles of rows
-  const int64_t tiles = (rows / fb::kExpertTileN + (m->n_slots < rows ? m->n_slots : rows)) * static_cast<int64_t>(p.m_blocks);
+  // a slot of c rows has at most ceil(c / tile) tiles of rows
+  const int64_t tiles = (rows / (e4m3 ? fb::kE4m3Rows : fb::kExpertTileN) + (m->n_slots < rows ? m->n_slots : rows)) * static_cast<int64_t>(p.m_blocks);
   if (tiles >= (int64_t{1} << 31)) return FB_ERR_UNSUPPORTED_SHAPE;
   CUtensorMap map_x, map_w;
   const CUtensorMapDataType type = e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
@@ -1211,27 +1214,27 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   bool ok;
   {
     const cuuint64_t size[2] = {K, static_cast<cuuint64_t>(x_rows)}, stride[1] = {row_bytes};
-    const cuuint32_t box[2] = {width, 1};                          // gathered row by row
+    const cuuint32_t box[2] = {width, fb::kTileLoadRows};
     ok = encode(&map_x, 2, x, size, stride, box);
   }
   if (swiglu) {                                                    // 16 rows of gate, 16 of up, ..
     const cuuint64_t size[5] = {K, 16, 2, static_cast<cuuint64_t>(p.n_out / 16), E};
     const cuuint64_t stride[4] = {row_bytes, row_bytes * p.n_out, row_bytes * 16, slot_bytes};
-    const cuuint32_t box[5] = {width, 16, 2, 4, 1};
+    const cuuint32_t box[5] = {width, 16, 2, e4m3 ? 8u : 4u, 1};
     ok = ok && encode(&map_w, 5, m->w, size, stride, box);
   } else {
     const cuuint64_t size[3] = {K, static_cast<cuuint64_t>(m->n), E}, stride[2] = {row_bytes, slot_bytes};
-    const cuuint32_t box[3] = {width, 128, 1};
+    const cuuint32_t box[3] = {width, e4m3 ? 256u : 128u, 1};
     ok = ok && encode(&map_w, 3, m->w, size, stride, box);
   }
   if (!ok) return FB_ERR_CUDA;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return FB_ERR_CUDA;
   const ExpertKernel kernel = expert_kernel(e4m3, swiglu, out_scale != nullptr);
-  const int64_t pairs = tiles < ctx->max_clusters[1] ? tiles : ctx->max_clusters[1];
+  const int64_t at_once = e4m3 ? ctx->n_sm : ctx->max_clusters[1], workers = tiles < at_once ? tiles : at_once;      // blocks, or pairs of them
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs), 1, 1);
+  cfg.gridDim = dim3(static_cast<unsigned>(e4m3 ? workers : 2 * workers), 1, 1);
   cfg.blockDim = dim3(fb::kExpertThreads, 1, 1);
   cfg.dynamicSmemBytes = kernel.smem;
   cfg.stream = static_cast<cudaStream_t>(stream_);
@@ -1243,7 +1246,7 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
+  cfg.numAttrs = e4m3 ? 1 : 2;
   const cudaError_t err = launch_refused(ctx) ? cudaErrorUnknown : cudaLaunchKernelEx(&cfg, kernel.fn, map_x, map_w, p);
   return err == cudaSuccess ? FB_OK : FB_ERR_CUDA;
 }

@@ -1,0 +1,331 @@
+// fb_expert_matmul with e4m3 operands and block scales: for every row p of slot s
+//     out[p][i] = act(sum over blocks b of 128 columns of  sx[row(p)][b] * sw_s[i / 128][b] * (q_x[row(p)][b] . q_w[i][b])).
+// The inner product of a block is a k-block of MMAs (tcgen05 kind::f8f6f4) with an accumulator of its own; the scaled sum
+// over the blocks is held in 32-bit registers, 128 rows x 256 columns in those of eight warps.
+//
+// Here the MMA's M side is x (128 rows) and its N side W (256 rows, with SwiGLU 16 of gate and 16 of up in turn): a TMEM
+// lane is a row of x, so a thread of the results warps has one row, whose scale is a register, and 128 rows of W, which
+// share one scale (with SwiGLU two).  The other way round - W on the M side in pairs of blocks, as for bf16, where counts
+// that are no multiple of the tile cost less - every column has a scale of its own, which each warp has to read from
+// shared memory for every k-block; that, tcgen05.ld in its 16-lane form and the way over two blocks at each hand-over took
+// 880 cycles per k-block whose MMAs take 512.
+//
+// One block per SM.  Warps: 0 loads by TMA, 1 issues the MMAs, 4-11 add up and store, 12-15 gather rows of x.  Two
+// accumulators of 256 columns: the MMAs fill one while the other is added up.
+#pragma once
+#include "fb_experts.cuh"
+
+namespace fb {
+
+constexpr int kE4m3Stages = 4;
+constexpr int kE4m3Rows = 128;                          // of x per tile
+constexpr uint32_t kE4m3XBytes = 128 * 128, kE4m3WBytes = 256 * 128, kE4m3StageBytes = kE4m3XBytes + kE4m3WBytes;
+constexpr int kE4m3Ahead = 4;                           // k-blocks whose scales are on their way
+constexpr uint32_t kE4m3WarpStaging = 32 * 64;          // 32 rows of 64 bytes
+constexpr uint32_t kE4m3StagingAt = kE4m3Stages * kE4m3StageBytes;
+constexpr uint32_t kE4m3Dynamic = kE4m3StagingAt + kExpertEpilogueWarps * kE4m3WarpStaging + 1024;
+
+struct ExpertE4m3Shared {
+  uint64_t full_bar[kE4m3Stages], empty_bar[kE4m3Stages], x_bar[kE4m3Stages];
+  uint64_t acc_full[2], acc_empty[2];
+  uint64_t top_bar[4];                                  // per quarter: its two warps' maxima are there
+  uint32_t tmem_base;
+  int32_t abort_flag;
+  float top[2][2][kE4m3Rows];                           // in turn; per half of the columns: a row's largest output
+  ExpertTiles tiles;
+};
+
+__device__ __forceinline__ void tma_load_rows(uint32_t dst, const void* tmap, uint32_t bar, int32_t c0, int32_t c1) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+               "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1)
+               : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, uint32_t bar, int32_t c0, int32_t c1, int32_t c2) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+               "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+               : "memory");
+}
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const void* tmap, uint32_t bar, int32_t c0, int32_t c1, int32_t c2, int32_t c3, int32_t c4) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
+      : "memory");
+}
+// e4m3 x e4m3 -> fp32, both operands K-major.
+__device__ __forceinline__ uint32_t umma_idesc_e4m3_f32(uint32_t M, uint32_t N) { return (1u << 4) | ((N >> 3) << 17) | ((M >> 4) << 24); }
+__device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(tmem_d),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void umma_commit_one(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// (d0, d1) += (a0, a1) * s
+__device__ __forceinline__ void fma_two(float& d0, float& d1, uint32_t a0, uint32_t a1, float s) {
+  asm("{\n.reg .b64 a, s, d;\nmov.b64 a, {%2, %3};\nmov.b64 s, {%4, %4};\nmov.b64 d, {%0, %1};\n"
+      "fma.rn.f32x2 d, a, s, d;\nmov.b64 {%0, %1}, d;\n}"
+      : "+f"(d0), "+f"(d1)
+      : "r"(a0), "r"(a1), "f"(s));
+}
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+  const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+  return lo | hi << 16;
+}
+
+template <bool kSwiglu, bool kQuantize>
+__global__ void __launch_bounds__(kExpertThreads, 1)
+fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+                             const __grid_constant__ ExpertParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ ExpertE4m3Shared sh;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
+  const int lane = threadIdx.x & 31;
+  const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  volatile int* abort_flag = &sh.abort_flag;
+  const bool gather = p.perm != nullptr;
+
+  if (threadIdx.x == 0) {
+    sh.abort_flag = 0;
+    for (int s = 0; s < kE4m3Stages; ++s) {
+      mbar_init(smem_u32(&sh.full_bar[s]), 1);
+      mbar_init(smem_u32(&sh.empty_bar[s]), 1);
+      mbar_init(smem_u32(&sh.x_bar[s]), 32 * kGatherWarps);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(smem_u32(&sh.acc_full[a]), 1);
+      mbar_init(smem_u32(&sh.acc_empty[a]), kExpertEpilogueWarps);
+    }
+    for (int q = 0; q < 4; ++q) mbar_init(smem_u32(&sh.top_bar[q]), 2);
+    fence_mbar_init();
+    prefetch_tensormap(&map_x);
+    prefetch_tensormap(&map_w);
+  }
+  if (warp == 1) {
+    tmem_alloc<1>(smem_u32(&sh.tmem_base), 512);
+    tmem_relinquish<1>();
+  }
+  tcgen05_fence_before();
+  __syncthreads();
+  tcgen05_fence_after();
+  pdl_wait();
+  pdl_launch_dependents();
+  const uint32_t tmem = sh.tmem_base;
+  expert_plan_tiles<kE4m3Rows>(sh.tiles, p);
+  const int total = sh.tiles.first_tile[p.n_slots] * p.m_blocks;
+  const int stride = static_cast<int>(gridDim.x), first = static_cast<int>(blockIdx.x);
+  const uint32_t base = p.slot_offsets != nullptr ? p.slot_offsets[0] : 0u;
+
+  // Registers: 256 threads with 208 and 256 with 48 are the 512 x 128 of the launch.
+  if (warp < kExpertFirstEpilogueWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    if (warp == 0) {
+      // ------------------------------------------------------------ TMA loads
+      const bool leader = elect_one();
+      uint32_t s = 0, phase = 0, fills = 0;
+      bool ok = true;
+      for (int g = first; g < total && ok; g += stride) {
+        const ExpertTile t = expert_tile<kE4m3Rows>(sh.tiles, p, g);
+        const int x_loads = gather ? 0 : (t.valid + kTileLoadRows - 1) / kTileLoadRows;      // rows behind the tile's last hold what they held
+        const uint32_t bytes = kE4m3WBytes + 128u * kTileLoadRows * static_cast<uint32_t>(x_loads);
+        for (int kb = 0; kb < p.num_kb; ++kb) {
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.empty_bar[s]), phase ^ 1u, abort_flag));
+          if (!ok) break;
+          const uint32_t x_dst = smem + s * kE4m3StageBytes, full = smem_u32(&sh.full_bar[s]);
+          if (leader) {
+            mbar_arrive_expect_tx(full, bytes);
+            if constexpr (kSwiglu) tma_load_5d(x_dst + kE4m3XBytes, &map_w, full, kb * 128, 0, 0, t.m * (kExpertTileM / 2) / 16, t.slot);
+            else tma_load_3d(x_dst + kE4m3XBytes, &map_w, full, kb * 128, t.m * kExpertTileM, t.slot);
+          }
+          __syncwarp();
+          if (lane < x_loads) tma_load_rows(x_dst + 128u * kTileLoadRows * lane, &map_x, full, kb * 128, t.row + kTileLoadRows * lane);
+          __syncwarp();
+          ++fills;
+          if (++s == kE4m3Stages) { s = 0; phase ^= 1u; }
+        }
+      }
+      if (!ok) {                                         // given up: the copies under way end before the block does
+        volatile int never = 0;
+        for (uint32_t f = fills > kE4m3Stages ? fills - kE4m3Stages : 0; f < fills; ++f)
+          mbar_wait(smem_u32(&sh.full_bar[f % kE4m3Stages]), (f / kE4m3Stages) & 1u, &never);
+      }
+    } else if (warp == 1) {
+      // ------------------------------------------------------------ MMAs
+      const bool leader = elect_one();
+      const uint32_t idesc = umma_idesc_e4m3_f32(128, 256);
+      uint32_t s = 0, phase = 0, used = 0;               // accumulators begun
+      bool ok = true;
+      for (int g = first; g < total && ok; g += stride) {
+        for (int kb = 0; kb < p.num_kb; ++kb) {
+          const uint32_t a = used & 1u, acc = tmem + a * 256u;
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.full_bar[s]), phase, abort_flag));
+          if (ok && gather) {
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.x_bar[s]), phase, abort_flag));
+            fence_proxy_async();
+          }
+          if (ok) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.acc_empty[a]), ((used >> 1) & 1u) ^ 1u, abort_flag));
+          if (!ok) break;
+          tcgen05_fence_after();
+          const uint32_t x_addr = smem + s * kE4m3StageBytes;
+          const uint64_t adesc = umma_smem_desc_sw128(x_addr), bdesc = umma_smem_desc_sw128(x_addr + kE4m3XBytes);
+          if (leader) {
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) umma_e4m3(acc, adesc + 2u * kk, bdesc + 2u * kk, idesc, kk != 0 ? 1u : 0u);      // 32 of K each
+            umma_commit_one(smem_u32(&sh.acc_full[a]));
+            umma_commit_one(smem_u32(&sh.empty_bar[s]));
+          }
+          __syncwarp();
+          ++used;
+          if (++s == kE4m3Stages) { s = 0; phase ^= 1u; }
+        }
+      }
+    }
+  } else if (warp >= kExpertFirstGatherWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    if (gather)
+      gather_rows<kE4m3Stages, kE4m3StageBytes>(p, total, first, stride, smem, sh.empty_bar, sh.x_bar, abort_flag,
+                                                [&](int g, int row0, int32_t (&r)[kGatherRows]) {
+        const ExpertTile t = expert_tile<kE4m3Rows>(sh.tiles, p, g);
+#pragma unroll
+        for (int i = 0; i < kGatherRows; ++i) r[i] = row0 + 16 * i < t.valid ? expert_x_row(p, base, t, row0 + 16 * i) : -1;
+      });
+  } else {
+    // -------------------------------------------------------------- sums and results
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    const int quarter = warp & 3, half = (warp - kExpertFirstEpilogueWarp) >> 2;     // TMEM lanes (rows of x); 128 columns each
+    const int row = quarter * 32 + lane;                 // of the tile
+    const uint32_t from = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + 128u * half;
+    const uint32_t staging = smem + kE4m3StagingAt + static_cast<uint32_t>(warp - kExpertFirstEpilogueWarp) * kE4m3WarpStaging;
+    uint32_t used = 0, tiles_done = 0;
+    bool ok = true;
+    // scales of the next k-blocks: this thread's row, and the blocks of W (gate and up; or this half's)
+    const float *xs = nullptr, *w0 = nullptr, *w1 = nullptr;
+    float v[kE4m3Ahead], a0[kE4m3Ahead], a1[kE4m3Ahead];
+    auto load = [&](int j, int kb) {
+      kb = min(kb, p.num_kb - 1);
+      v[j] = xs[kb];
+      a0[j] = w0[kb];
+      if constexpr (kSwiglu) a1[j] = w1[kb];
+    };
+    auto begin = [&](const ExpertTile& t) {
+      xs = p.x_scale + static_cast<size_t>(expert_x_row(p, base, t, row)) * p.scale_k;
+      const float* ws = p.w_scale + static_cast<size_t>(t.slot) * p.w_scale_slot;
+      const int blocks = (p.n_out + 127) / 128;          // (the second half of a tile may lie behind the last row of W: not stored)
+      w0 = ws + static_cast<size_t>(kSwiglu ? t.m : min(2 * t.m + half, blocks - 1)) * p.scale_k;
+      if constexpr (kSwiglu) w1 = w0 + static_cast<size_t>(blocks) * p.scale_k;
+#pragma unroll
+      for (int j = 0; j < kE4m3Ahead; ++j) load(j, j);
+    };
+    // 64 bytes of each of the warp's 32 rows, from `value`, to column `first_byte` of out
+    auto store = [&](const ExpertTile& t, size_t row_bytes, size_t first_byte, const uint32_t (&value)[16]) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        st_shared_v4(staging + static_cast<uint32_t>(lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)), value[4 * i], value[4 * i + 1],
+                     value[4 * i + 2], value[4 * i + 3]);
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 2), unit = lane & 3;
+        const uint4 w = ld_shared_v4(staging + static_cast<uint32_t>(r * 64 + ((unit ^ ((r >> 1) & 3)) << 4)));
+        if (quarter * 32 + r < t.valid && first_byte + 16 * unit < row_bytes)
+          *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.out) + static_cast<size_t>(t.row + quarter * 32 + r) * row_bytes + first_byte + 16 * unit) = w;
+      }
+      __syncwarp();
+    };
+    ExpertTile t;
+    if (first < total) {
+      t = expert_tile<kE4m3Rows>(sh.tiles, p, first);
+      begin(t);
+    }
+    for (int g = first; g < total && ok; g += stride) {
+      float acc[128];                                    // SwiGLU: 16 gate, 16 up, ..
+#pragma unroll
+      for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
+      for (int kb0 = 0; kb0 < p.num_kb && ok; kb0 += kE4m3Ahead) {
+#pragma unroll
+        for (int j = 0; j < kE4m3Ahead; ++j) {
+          if (kb0 + j >= p.num_kb || !ok) break;
+          const float s0 = v[j] * a0[j], s1 = kSwiglu ? v[j] * a1[j] : s0;
+          load(j, kb0 + j + kE4m3Ahead);
+          const uint32_t a = used & 1u;
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.acc_full[a]), (used >> 1) & 1u, abort_flag));
+          if (!ok) break;
+          tcgen05_fence_after();
+          // 16 columns are added while the next 16 are on their way
+          uint32_t r[2][16];
+          tmem_ld_32x32b_x16(from + 256u * a, r[0]);
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            tmem_ld_wait();
+            if (c < 7) {
+              tmem_ld_32x32b_x16(from + 256u * a + 16u * (c + 1), r[(c + 1) & 1]);
+            } else {
+              tcgen05_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(smem_u32(&sh.acc_empty[a]));
+            }
+#pragma unroll
+            for (int i = 0; i < 16; i += 2)
+              fma_two(acc[16 * c + i], acc[16 * c + i + 1], r[c & 1][i], r[c & 1][i + 1], (c & 1) == 0 ? s0 : s1);
+          }
+          ++used;
+        }
+      }
+      if (!ok) break;
+      const ExpertTile done = t;
+      if (g + stride < total) {                          // the next tile's first scales arrive under the stores
+        t = expert_tile<kE4m3Rows>(sh.tiles, p, g + stride);
+        begin(t);
+      }
+      if constexpr (kSwiglu) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[16 * c + i] = swiglu(acc[32 * c + i], acc[32 * c + 16 + i]);
+      }
+      uint32_t value[16];
+      if constexpr (!kQuantize) {
+        constexpr int kPasses = kSwiglu ? 2 : 4;         // of 32 columns
+#pragma unroll
+        for (int c = 0; c < kPasses; ++c) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) value[i] = pack_bf16(acc[32 * c + 2 * i], acc[32 * c + 2 * i + 1]);
+          store(done, 2 * static_cast<size_t>(p.n_out), 2 * static_cast<size_t>(done.m * 32 * kPasses * 2 + half * 32 * kPasses + 32 * c), value);
+        }
+      } else {
+        // A row's 128 outputs are in the two warps of its quarter.  Two sets in turn: who writes a set again has seen the
+        // other warp at the barrier of the set between.
+        float top = 0x1p-100f;                           // smallest scale: see fb_quantize_rows
+#pragma unroll
+        for (int i = 0; i < 64; ++i) top = fmaxf(top, fabsf(acc[i]));
+        float (&tops)[2][kE4m3Rows] = sh.top[tiles_done & 1u];
+        tops[half][row] = top;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh.top_bar[quarter]));
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.top_bar[quarter]), tiles_done & 1u, abort_flag));
+        if (!ok) break;
+        top = fmaxf(top, tops[half ^ 1][row]);
+        const float inv = 448.0f / top;
+        if (half == 0 && row < done.valid) p.out_scale[static_cast<size_t>(done.row + row) * ((p.n_out + 127) / 128) + done.m] = top / 448.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) value[i] = pack_e4m3(acc[4 * i] * inv, acc[4 * i + 1] * inv, acc[4 * i + 2] * inv, acc[4 * i + 3] * inv);
+        store(done, static_cast<size_t>(p.n_out), static_cast<size_t>(done.m * 128 + half * 64), value);
+      }
+      ++tiles_done;
+    }
+  }
+
+  // ---------------------------------------------------------------- teardown
+  tcgen05_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && sh.abort_flag) atomicCAS(p.status, 0, FB_ERR_TIMEOUT);
+  if (warp == 1) {
+    tcgen05_fence_after();
+    tmem_dealloc<1>(tmem, 512);
+  }
+}
+
+}  // namespace fb
