@@ -1153,7 +1153,7 @@ fb_status fb_quantize_rows(fb_ctx* ctx, const void* x, int64_t rows, int32_t n, 
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return FB_ERR_CUDA;
   const int64_t blocks = (rows * blocks_k + per_block - 1) / per_block;
-  return launch_counted(ctx, fb::fb_quantize_rows_kernel, static_cast<int>(blocks), fb::kQuantizeThreads, kAnyShare,
+  return launch_counted(ctx, n % 128 == 0 ? fb::fb_quantize_rows_kernel<true> : fb::fb_quantize_rows_kernel<false>, static_cast<int>(blocks), fb::kQuantizeThreads, kAnyShare,
                         static_cast<cudaStream_t>(stream_), static_cast<const __nv_bfloat16*>(x), static_cast<long long>(rows), n,
                         blocks_k, static_cast<uint8_t*>(q), scale) == cudaSuccess ? FB_OK : FB_ERR_CUDA;
 }

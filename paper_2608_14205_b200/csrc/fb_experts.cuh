@@ -42,12 +42,12 @@ constexpr int kExpertFirstGatherWarp = 12;
 constexpr int kGatherWarps = 4;
 constexpr int kGatherRows = 8;                          // rows per thread: 128 rows / 4 warps / 4 rows per copy of a warp
 constexpr int kTileLoadRows = 16;                       // rows of x per TMA load
-constexpr int kExpertStages = 6;
+constexpr uint32_t kExpertRingBytes = 6 * 32768;         // stages of 128 rows of W and as many of x as the largest tile has
+constexpr int kExpertStages = 12;                       // at most
 constexpr int kExpertTileM = 256;                       // rows of W per pair
 constexpr int kExpertTileN = 256;                       // rows of x per tile at most
 constexpr int kExpertStepN = 32;                        // (the MMA of a pair takes N in steps of 32)
-constexpr uint32_t kExpertWBytes = 128 * 128;           // a block's part of a stage: 128 rows of W ..
-constexpr uint32_t kExpertStageBytes = 2 * kExpertWBytes;   // .. and up to 128 rows of x, 128 bytes each
+constexpr uint32_t kExpertWBytes = 128 * 128;           // 128 rows of W, 128 bytes each
 constexpr int kBand = 8;                                // tiles of x that share a walk over W
 
 struct ExpertParams {
@@ -69,6 +69,7 @@ struct ExpertParams {
 };
 
 struct ExpertTiles {
+  int32_t most;                                         // rows of x in the largest tile
   int32_t warp_sums[kExpertThreads / 32];
   int32_t first_tile[FB_MAX_EXPERTS + 1];               // tiles of x before this slot's
   int32_t first_row[FB_MAX_EXPERTS];
@@ -145,6 +146,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+  const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+  return lo | hi << 16;
+}
 __device__ __forceinline__ float swiglu(float g, float u) { return __fdividef(g, 1.0f + __expf(-g)) * u; }
 
 // ---------------------------------------------------------------- tiles
@@ -185,6 +191,7 @@ __device__ __forceinline__ void expert_plan_tiles(ExpertTiles& sh, const ExpertP
     sh.first_row[e] = first;
     sh.count[e] = count;
     tiles = expert_tiles<kRows>(count);
+    if (tiles > 0) atomicMax(&sh.most, expert_tile_rows<kRows>(count, tiles));
   }
   int sum = tiles;
 #pragma unroll
@@ -243,15 +250,16 @@ struct ExpertLayout {
   // rows of 16 (SwiGLU) or 32 numbers with a pad that keeps eight rows in different banks
   static constexpr int kRowBytes = kSwiglu ? 48 : 80;
   static constexpr int kWarpStaging = 32 * kRowBytes;
-  static constexpr uint32_t kStagingAt = kExpertStages * kExpertStageBytes;
+  static constexpr uint32_t kStagingAt = kExpertRingBytes;
   static constexpr uint32_t kDynamic = kStagingAt + kExpertEpilogueWarps * kWarpStaging + 1024;
 };
 
 // The gather warps' part of a kernel: for every k-block of every tile, rows(g, i, r) gives the row numbers of this thread
 // (row0 + 16 i of the block's 128; false: not needed), whose 16 bytes each go to the stage's tile of 128-byte rows in the
 // 128-byte swizzle.  x_bar[s] counts the threads whose copies are complete.
-template <int kStages, uint32_t kStageBytes, typename Rows>
-__device__ __forceinline__ void gather_rows(const ExpertParams& p, int total, int first, int stride, uint32_t x_tiles, uint64_t* empty_bar,
+template <typename Rows>
+__device__ __forceinline__ void gather_rows(const ExpertParams& p, int total, int first, int stride, uint32_t x_tiles, uint32_t stages,
+                                            uint32_t stage_bytes, uint64_t* empty_bar,
                                             uint64_t* x_bar, volatile int* abort_flag, Rows rows_of) {
   const int lane = threadIdx.x & 31, unit = lane & 7;
   const int row0 = (static_cast<int>(threadIdx.x >> 5) - kExpertFirstGatherWarp) * 4 + (lane >> 3);
@@ -275,10 +283,10 @@ __device__ __forceinline__ void gather_rows(const ExpertParams& p, int total, in
 #pragma unroll
       for (int i = 0; i < kGatherRows; ++i)
         if (rows[i] >= 0)
-          cp_async_16(to + s * kStageBytes + 2048u * i, src + static_cast<uint64_t>(static_cast<uint32_t>(rows[i])) * row_bytes, inside ? 16u : 0u);
+          cp_async_16(to + s * stage_bytes + 2048u * i, src + static_cast<uint64_t>(static_cast<uint32_t>(rows[i])) * row_bytes, inside ? 16u : 0u);
       cp_async_arrive(smem_u32(&x_bar[s]));
       if (kb == 0 && g + stride < total) rows_of(g + stride, row0, next_rows);      // these numbers arrive meanwhile
-      if (++s == kStages) { s = 0; phase ^= 1u; }
+      if (++s == stages) { s = 0; phase ^= 1u; }
     }
   }
   cp_async_wait_all();
@@ -301,6 +309,7 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
 
   if (threadIdx.x == 0) {
     sh.abort_flag = 0;
+    sh.tiles.most = 0;
     for (int s = 0; s < kExpertStages; ++s) {
       mbar_init(smem_u32(&sh.full_bar[s]), gather ? 2 : 1);        // the loads; the odd block's gathered rows
       mbar_init(smem_u32(&sh.empty_bar[s]), 1);
@@ -329,6 +338,9 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
   const int total = sh.tiles.first_tile[p.n_slots] * p.m_blocks;
   const int stride = static_cast<int>(gridDim.x) / 2, first = static_cast<int>(blockIdx.x) / 2;
   const uint32_t base = p.slot_offsets != nullptr ? p.slot_offsets[0] : 0u;
+  // Few rows per tile leave room for more stages: what is under way is W, and a launch of few tiles has few blocks to ask for it.
+  const uint32_t stage_bytes = kExpertWBytes + 64u * static_cast<uint32_t>(max(sh.tiles.most, kExpertStepN));
+  const uint32_t stages = min(kExpertRingBytes / stage_bytes, static_cast<uint32_t>(kExpertStages));
 
   if (warp == 0) {
     // -------------------------------------------------------------- TMA loads
@@ -342,7 +354,7 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
       for (int kb = 0; kb < p.num_kb; ++kb) {
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.empty_bar[s]), phase ^ 1u, abort_flag));
         if (!ok) break;
-        const uint32_t w_dst = smem + s * kExpertStageBytes, x_dst = w_dst + kExpertWBytes;
+        const uint32_t w_dst = smem + s * stage_bytes, x_dst = w_dst + kExpertWBytes;
         const uint32_t full = map_to_cta(smem_u32(&sh.full_bar[s]), 0u);
         if (leader) {
           if (rank == 0) mbar_arrive_expect_tx(smem_u32(&sh.full_bar[s]), bytes);
@@ -356,13 +368,13 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
           tma_load_rows_pair(x_dst + 128u * kTileLoadRows * lane, &map_x, full, kb * kStepK, x_row);
         __syncwarp();
         ++fills;
-        if (++s == kExpertStages) { s = 0; phase ^= 1u; }
+        if (++s == stages) { s = 0; phase ^= 1u; }
       }
     }
     if (!ok && rank == 0) {                              // given up: the copies under way end before the block does
       volatile int never = 0;
-      for (uint32_t f = fills > kExpertStages ? fills - kExpertStages : 0; f < fills; ++f)
-        mbar_wait(smem_u32(&sh.full_bar[f % kExpertStages]), (f / kExpertStages) & 1u, &never);
+      for (uint32_t f = fills > stages ? fills - stages : 0; f < fills; ++f)
+        mbar_wait(smem_u32(&sh.full_bar[f % stages]), (f / stages) & 1u, &never);
     }
   } else if (warp == 1 && rank == 0) {
     // -------------------------------------------------------------- MMAs
@@ -382,7 +394,7 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
         }
         if (!ok) break;
         tcgen05_fence_after();
-        const uint32_t w_addr = smem + s * kExpertStageBytes;
+        const uint32_t w_addr = smem + s * stage_bytes;
         const uint64_t adesc = umma_smem_desc_sw128(w_addr), bdesc = umma_smem_desc_sw128(w_addr + kExpertWBytes);
         if (leader) {
 #pragma unroll
@@ -392,7 +404,7 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
           if (kb == p.num_kb - 1) umma_commit_pair(smem_u32(&sh.acc_full[a]), 0u);
         }
         __syncwarp();
-        if (++s == kExpertStages) { s = 0; phase ^= 1u; }
+        if (++s == stages) { s = 0; phase ^= 1u; }
       }
       ++used;
     }
@@ -407,11 +419,11 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
         fence_proxy_async();
         if (lane == 0) mbar_arrive_pair(smem_u32(&sh.full_bar[s]), 0u);
         __syncwarp();
-        if (++s == kExpertStages) { s = 0; phase ^= 1u; }
+        if (++s == stages) { s = 0; phase ^= 1u; }
       }
   } else if (warp >= kExpertFirstGatherWarp) {
     if (gather)
-      gather_rows<kExpertStages, kExpertStageBytes>(p, total, first, stride, smem + kExpertWBytes, sh.empty_bar, sh.x_bar, abort_flag,
+      gather_rows(p, total, first, stride, smem + kExpertWBytes, stages, stage_bytes, sh.empty_bar, sh.x_bar, abort_flag,
                                                     [&](int g, int row0, int32_t (&r)[kGatherRows]) {
         const ExpertTile t = expert_tile<kExpertTileN>(sh.tiles, p, g);
 #pragma unroll
@@ -483,10 +495,12 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
 
 // ---------------------------------------------------------------- rows to e4m3 with block scales
 // Half a warp per block of 128 columns: a = max(max |x|, 2^-100), s = a / 448, q = x * (448 / a) rounded to e4m3.
-// HBM bound: 3 bytes per number.
+// HBM bound: 3 bytes per number.  A thread has kQuantizeUnroll loads of 16 bytes, of consecutive blocks, under way together.
 constexpr int kQuantizeThreads = 256;
 constexpr int kQuantizeUnroll = 4;
 
+// kWhole: n is a multiple of 128, so block b is the numbers 128 b .. 128 b + 127 of x, whatever its row.
+template <bool kWhole>
 __global__ void __launch_bounds__(kQuantizeThreads)
 fb_quantize_rows_kernel(const __nv_bfloat16* __restrict__ x, long long rows, int n, int blocks_k, uint8_t* __restrict__ q,
                         float* __restrict__ scale) {
@@ -497,36 +511,43 @@ fb_quantize_rows_kernel(const __nv_bfloat16* __restrict__ x, long long rows, int
   const long long item0 = (static_cast<long long>(blockIdx.x) * (kQuantizeThreads / 16) + (threadIdx.x >> 4)) * kQuantizeUnroll;
   uint4 v[kQuantizeUnroll];
   long long at[kQuantizeUnroll];
-#pragma unroll
-  for (int i = 0; i < kQuantizeUnroll; ++i) {
-    const long long item = item0 + i, row = item / blocks_k;
-    const int column = static_cast<int>(item - row * blocks_k) * 128 + lane * 8;
-    at[i] = (item < items && column < n) ? row * n + column : -1;
-    v[i] = make_uint4(0, 0, 0, 0);
-    if (at[i] >= 0) v[i] = __ldcs(reinterpret_cast<const uint4*>(x + at[i]));
+  long long row = 0;
+  int block = 0;
+  if constexpr (!kWhole) {
+    row = item0 / blocks_k;
+    block = static_cast<int>(item0 - row * blocks_k);
   }
 #pragma unroll
   for (int i = 0; i < kQuantizeUnroll; ++i) {
-    float f[8];
+    if constexpr (kWhole) {
+      at[i] = item0 + i < items ? (item0 + i) * 128 + lane * 8 : -1;
+    } else {
+      const int column = block * 128 + lane * 8;
+      at[i] = (item0 + i < items && column < n) ? row * n + column : -1;
+      if (++block == blocks_k) { block = 0; ++row; }
+    }
+    v[i] = make_uint4(0, 0, 0, 0);
+    if (at[i] >= 0) v[i] = __ldcs(reinterpret_cast<const uint4*>(x + at[i]));
+  }
+  float scales = 0.0f;                                   // lane i keeps that of block i
+#pragma unroll
+  for (int i = 0; i < kQuantizeUnroll; ++i) {
     const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+    float f[8], top = 0x1p-100f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) { f[2 * j] = __uint_as_float(w[j] << 16); f[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
-    float top = 0x1p-100f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(f[j]));
 #pragma unroll
     for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    if (lane == i) scales = top;
     const float inv = 448.0f / top;
     uint32_t packed[2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * j] * inv, f[4 * j + 1] * inv), __NV_SATFINITE, __NV_E4M3);
-      const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * j + 2] * inv, f[4 * j + 3] * inv), __NV_SATFINITE, __NV_E4M3);
-      packed[j] = lo | hi << 16;
-    }
+    for (int j = 0; j < 2; ++j) packed[j] = pack_e4m3(f[4 * j] * inv, f[4 * j + 1] * inv, f[4 * j + 2] * inv, f[4 * j + 3] * inv);
     if (at[i] >= 0) *reinterpret_cast<uint2*>(q + at[i]) = make_uint2(packed[0], packed[1]);
-    if (lane == 0 && item0 + i < items) scale[item0 + i] = top / 448.0f;
   }
+  if (lane < kQuantizeUnroll && item0 + lane < items) scale[item0 + lane] = scales / 448.0f;
 }
 
 // ---------------------------------------------------------------- weighted sum of a token's rows

@@ -70,12 +70,6 @@ __device__ __forceinline__ void fma_two(float& d0, float& d1, uint32_t a0, uint3
       : "+f"(d0), "+f"(d1)
       : "r"(a0), "r"(a1), "f"(s));
 }
-__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
-  const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
-  const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
-  return lo | hi << 16;
-}
-
 template <bool kSwiglu, bool kQuantize>
 __global__ void __launch_bounds__(kExpertThreads, 1)
 fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
@@ -90,6 +84,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
 
   if (threadIdx.x == 0) {
     sh.abort_flag = 0;
+    sh.tiles.most = 0;
     for (int s = 0; s < kE4m3Stages; ++s) {
       mbar_init(smem_u32(&sh.full_bar[s]), 1);
       mbar_init(smem_u32(&sh.empty_bar[s]), 1);
@@ -186,7 +181,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
   } else if (warp >= kExpertFirstGatherWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (gather)
-      gather_rows<kE4m3Stages, kE4m3StageBytes>(p, total, first, stride, smem, sh.empty_bar, sh.x_bar, abort_flag,
+      gather_rows(p, total, first, stride, smem, kE4m3Stages, kE4m3StageBytes, sh.empty_bar, sh.x_bar, abort_flag,
                                                 [&](int g, int row0, int32_t (&r)[kGatherRows]) {
         const ExpertTile t = expert_tile<kE4m3Rows>(sh.tiles, p, g);
 #pragma unroll
