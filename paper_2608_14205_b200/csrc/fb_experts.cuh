@@ -19,8 +19,8 @@
 // W, whose size is a multiple of what a tile needs in all practice; its N side, which goes in steps of 32, is x, so that
 // the ragged counts of the slots (a few rows in decode, any number in prefill) cost what they have, not what a tile holds:
 // a slot with 300 rows is two tiles of 160, not two of 256.
-// Warps: 0 loads by TMA, 1 issues the MMAs (even block) or passes on that gathered rows are there (odd block), 4-11 take
-// the accumulators out while the next tile's MMAs run, 12-15 gather.  TMEM lanes are rows of W, columns rows of x; the
+// Warps: 0 loads by TMA, 1 issues the MMAs (even block), 2 passes on that gathered rows are there, 4-11 take the
+// accumulators out while the next tile's MMAs run, 12-15 gather.  TMEM lanes are rows of W, columns rows of x; the
 // 16x256b form of tcgen05.ld gives a thread the same columns of lanes r and r + 16, where W's tile has its gate row r and
 // up row r side by side (the tensor map interleaves them 16 by 16), so SwiGLU needs no exchange.
 #pragma once
@@ -42,6 +42,7 @@ constexpr int kExpertFirstGatherWarp = 12;
 constexpr int kGatherWarps = 4;
 constexpr int kGatherRows = 8;                          // rows per thread: 128 rows / 4 warps / 4 rows per copy of a warp
 constexpr int kTileLoadRows = 16;                       // rows of x per TMA load
+constexpr int kNoRow = -2, kZeroRow = -1;
 constexpr uint32_t kExpertRingBytes = 6 * 32768;         // stages of 128 rows of W and as many of x as the largest tile has
 constexpr int kExpertStages = 12;                       // at most
 constexpr int kExpertTileM = 256;                       // rows of W per pair
@@ -70,6 +71,7 @@ struct ExpertParams {
 
 struct ExpertTiles {
   int32_t most;                                         // rows of x in the largest tile
+  int32_t warp_most[kExpertThreads / 32];
   int32_t warp_sums[kExpertThreads / 32];
   int32_t first_tile[FB_MAX_EXPERTS + 1];               // tiles of x before this slot's
   int32_t first_row[FB_MAX_EXPERTS];
@@ -173,13 +175,14 @@ __device__ __forceinline__ int expert_tiles(int c) {
 
 // All threads: the tiles of every slot.  Counts that are no prefix sums below `rows` are reported and their rows left out.
 template <int kRows>
-__device__ __forceinline__ void expert_plan_tiles(ExpertTiles& sh, const ExpertParams& p) {
+__device__ __forceinline__ void expert_plan_tiles(ExpertTiles& sh, const ExpertParams& p, uint32_t& base) {
   const int e = threadIdx.x, lane = e & 31, warp = e >> 5;
-  int tiles = 0;
+  int tiles = 0, most = 0;
+  base = p.slot_offsets != nullptr ? p.slot_offsets[0] : 0u;
   if (e < p.n_slots) {
     int first = 0, count = p.rows;
     if (p.slot_offsets != nullptr) {
-      const uint32_t base = p.slot_offsets[0], lo = p.slot_offsets[e], hi = p.slot_offsets[e + 1];
+      const uint32_t lo = p.slot_offsets[e], hi = p.slot_offsets[e + 1];
       if (base <= lo && lo <= hi && hi - base <= static_cast<uint32_t>(p.rows)) {
         first = static_cast<int>(lo - base);
         count = static_cast<int>(hi - lo);
@@ -188,10 +191,10 @@ __device__ __forceinline__ void expert_plan_tiles(ExpertTiles& sh, const ExpertP
         atomicCAS(p.status, 0, FB_ERR_RANGE);
       }
     }
+    tiles = expert_tiles<kRows>(count);
+    if (tiles > 0) most = expert_tile_rows<kRows>(count, tiles);
     sh.first_row[e] = first;
     sh.count[e] = count;
-    tiles = expert_tiles<kRows>(count);
-    if (tiles > 0) atomicMax(&sh.most, expert_tile_rows<kRows>(count, tiles));
   }
   int sum = tiles;
 #pragma unroll
@@ -199,50 +202,66 @@ __device__ __forceinline__ void expert_plan_tiles(ExpertTiles& sh, const ExpertP
     const int v = __shfl_up_sync(0xffffffffu, sum, d);
     if (lane >= d) sum += v;
   }
-  if (lane == 31) sh.warp_sums[warp] = sum;
+  most = __reduce_max_sync(0xffffffffu, most);
+  if (lane == 31) { sh.warp_sums[warp] = sum; sh.warp_most[warp] = most; }
   __syncthreads();
-  for (int w = 0; w < warp; ++w) sum += sh.warp_sums[w];
+  const int w = lane < kExpertThreads / 32 ? sh.warp_sums[lane] : 0;
+  sum += __reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
   if (e < p.n_slots) sh.first_tile[e + 1] = sum;
-  if (e == 0) sh.first_tile[0] = 0;
+  if (e == 0) {
+    sh.first_tile[0] = 0;
+    most = 0;
+    for (int i = 0; i < (p.n_slots + 31) / 32; ++i) most = max(most, sh.warp_most[i]);
+    sh.most = most;
+  }
   __syncthreads();
 }
 
 // Tile number g: slot by slot; inside a slot bands of up to kBand tiles of x, which walk over W together (a tile of W is
-// then read by the band's tiles at about the same time, and the band's rows of x stay in L2).
+// then read by the band's tiles at about the same time, and the band's rows of x stay in L2).  A whole warp asks, for
+// numbers that rise: from_slot is the slot of the one before (0 at first), 32 slots are looked at at a time.
 template <int kRows>
-__device__ __forceinline__ ExpertTile expert_tile(const ExpertTiles& sh, const ExpertParams& p, int g) {
-  int lo = 0, hi = p.n_slots;                            // first_tile[lo] * m_blocks <= g < first_tile[hi] * m_blocks
-  const int tile = g / p.m_blocks;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (sh.first_tile[mid] <= tile) lo = mid; else hi = mid;
+__device__ __forceinline__ ExpertTile expert_tile(const ExpertTiles& sh, const ExpertParams& p, int g, int& from_slot) {
+  const int tile = g / p.m_blocks, lane = threadIdx.x & 31;
+  int slot = from_slot;
+  for (;;) {                                             // first_tile[slot] <= tile < first_tile[slot + 1]
+    const int at = slot + 1 + lane;
+    const unsigned past = __ballot_sync(0xffffffffu, at >= p.n_slots || sh.first_tile[at] > tile);
+    if (past != 0) { slot += __ffs(past) - 1; break; }
+    slot += 32;
   }
+  from_slot = slot;
   ExpertTile t;
-  t.slot = lo;
-  const int first = sh.first_tile[lo], tiles = sh.first_tile[lo + 1] - first;
-  int r = g - first * p.m_blocks;
-  const int band = r / (kBand * p.m_blocks);
-  const int width = min(kBand, tiles - band * kBand);
-  r -= band * kBand * p.m_blocks;
-  t.m = r / width;
-  const int j = band * kBand + r - t.m * width;
-  const int count = sh.count[lo], per = expert_tile_rows<kRows>(count, tiles);
-  t.row = sh.first_row[lo] + j * per;
+  t.slot = slot;
+  const int first = sh.first_tile[slot], tiles = sh.first_tile[slot + 1] - first;
+  int r = g - first * p.m_blocks, j = 0, width = tiles;
+  if (tiles > kBand) {
+    j = r / (kBand * p.m_blocks) * kBand;
+    width = min(kBand, tiles - j);
+    r -= j * p.m_blocks;
+  }
+  t.m = r;
+  if (width > 1) {
+    t.m = r / width;
+    j += r - t.m * width;
+  }
+  const int count = sh.count[slot], per = expert_tile_rows<kRows>(count, tiles);
+  t.row = sh.first_row[slot] + j * per;
   t.valid = min(per, count - j * per);
   t.n = round_up_n(t.valid);
   return t;
 }
 
-// The row of x at position `row` (counted from slot_offsets[0]); rows behind a tile's last repeat that one.
+// The row of x that is row i of a tile, or kZeroRow behind the tile's last one.  (Zeros there, not whatever was there or a
+// repeated row: the results are not stored, but products of zeros take less power, and the power limit sets the clock.)
 __device__ __forceinline__ int expert_x_row(const ExpertParams& p, uint32_t base, const ExpertTile& t, int i) {
-  const int row = t.row + min(i, t.valid - 1);
-  int x = row;
-  if (p.perm != nullptr) x = p.perm[static_cast<size_t>(base) + row] / p.k;
+  int x = t.row + min(i, t.valid - 1);                   // counted from slot_offsets[0]; no branch: a thread's loads go out together
+  if (p.perm != nullptr) x = p.perm[static_cast<size_t>(base) + x] / p.k;
   if (static_cast<unsigned>(x) >= static_cast<unsigned>(p.x_rows)) {
     atomicCAS(p.status, 0, FB_ERR_RANGE);
     x = 0;
   }
-  return x;
+  return i < t.valid ? x : kZeroRow;
 }
 
 template <bool kSwiglu>
@@ -254,9 +273,9 @@ struct ExpertLayout {
   static constexpr uint32_t kDynamic = kStagingAt + kExpertEpilogueWarps * kWarpStaging + 1024;
 };
 
-// The gather warps' part of a kernel: for every k-block of every tile, rows(g, i, r) gives the row numbers of this thread
-// (row0 + 16 i of the block's 128; false: not needed), whose 16 bytes each go to the stage's tile of 128-byte rows in the
-// 128-byte swizzle.  x_bar[s] counts the threads whose copies are complete.
+// The gather warps' part of a kernel: for every k-block of every tile, rows_of(g, row0, r) gives the row numbers of this
+// thread's rows row0 + 16 i of the block's 128 (kNoRow: nothing is written, kZeroRow: zeros are), whose 16 bytes each go to
+// the stage's tile of 128-byte rows in the 128-byte swizzle.  x_bar[s] counts the threads whose copies are complete and the warps.
 template <typename Rows>
 __device__ __forceinline__ void gather_rows(const ExpertParams& p, int total, int first, int stride, uint32_t x_tiles, uint32_t stages,
                                             uint32_t stage_bytes, uint64_t* empty_bar,
@@ -267,13 +286,16 @@ __device__ __forceinline__ void gather_rows(const ExpertParams& p, int total, in
   const uint32_t to = x_tiles + static_cast<uint32_t>(row0 * 128 + ((unit ^ (row0 & 7)) << 4));        // (16 i rows on: same swizzle)
   uint32_t s = 0, phase = 0;
   bool ok = true;
-  int32_t rows[kGatherRows], next_rows[kGatherRows];                    // -1: none
+  int32_t rows[kGatherRows], next_rows[kGatherRows];
 #pragma unroll
-  for (int i = 0; i < kGatherRows; ++i) next_rows[i] = -1;
+  for (int i = 0; i < kGatherRows; ++i) next_rows[i] = kNoRow;
   if (first < total) rows_of(first, row0, next_rows);
   for (int g = first; g < total && ok; g += stride) {
 #pragma unroll
     for (int i = 0; i < kGatherRows; ++i) rows[i] = next_rows[i];
+    bool any_zero = false;
+#pragma unroll
+    for (int i = 0; i < kGatherRows; ++i) any_zero = any_zero || rows[i] == kZeroRow;
     for (int kb = 0; kb < p.num_kb; ++kb) {
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&empty_bar[s]), phase ^ 1u, abort_flag));
       if (!ok) break;
@@ -284,12 +306,36 @@ __device__ __forceinline__ void gather_rows(const ExpertParams& p, int total, in
       for (int i = 0; i < kGatherRows; ++i)
         if (rows[i] >= 0)
           cp_async_16(to + s * stage_bytes + 2048u * i, src + static_cast<uint64_t>(static_cast<uint32_t>(rows[i])) * row_bytes, inside ? 16u : 0u);
+      if (kb < static_cast<int>(stages) && any_zero) {   // zeros stay for the tile's later uses of the stage
+#pragma unroll
+        for (int i = 0; i < kGatherRows; ++i)
+          if (rows[i] == kZeroRow) st_shared_v4(to + s * stage_bytes + 2048u * i, 0u, 0u, 0u, 0u);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&x_bar[s]));   // (the zeros; the copies report for themselves)
       cp_async_arrive(smem_u32(&x_bar[s]));
       if (kb == 0 && g + stride < total) rows_of(g + stride, row0, next_rows);      // these numbers arrive meanwhile
       if (++s == stages) { s = 0; phase ^= 1u; }
     }
   }
   cp_async_wait_all();
+}
+
+// One warp's part: gathered rows that have arrived are made visible to the tensor core and reported.
+template <typename Arrive>
+__device__ __forceinline__ void pass_on_rows(const ExpertParams& p, int total, int first, int stride, uint32_t stages, uint64_t* x_bar,
+                                             volatile int* abort_flag, Arrive arrive) {
+  uint32_t s = 0, phase = 0;
+  bool ok = true;
+  for (int g = first; g < total && ok; g += stride)
+    for (int kb = 0; kb < p.num_kb; ++kb) {
+      ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&x_bar[s]), phase, abort_flag));
+      if (!ok) break;
+      fence_proxy_async();
+      if ((threadIdx.x & 31) == 0) arrive(s);
+      __syncwarp();
+      if (++s == stages) { s = 0; phase ^= 1u; }
+    }
 }
 
 template <bool kSwiglu>
@@ -309,11 +355,10 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
 
   if (threadIdx.x == 0) {
     sh.abort_flag = 0;
-    sh.tiles.most = 0;
     for (int s = 0; s < kExpertStages; ++s) {
-      mbar_init(smem_u32(&sh.full_bar[s]), gather ? 2 : 1);        // the loads; the odd block's gathered rows
+      mbar_init(smem_u32(&sh.full_bar[s]), gather ? 3 : 1);        // the TMA loads; each block's gathered rows
       mbar_init(smem_u32(&sh.empty_bar[s]), 1);
-      mbar_init(smem_u32(&sh.x_bar[s]), 32 * kGatherWarps);
+      mbar_init(smem_u32(&sh.x_bar[s]), 33 * kGatherWarps);
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(smem_u32(&sh.acc_full[a]), 1);
@@ -334,10 +379,11 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
   pdl_wait();
   pdl_launch_dependents();
   const uint32_t tmem = sh.tmem_base;
-  expert_plan_tiles<kExpertTileN>(sh.tiles, p);
+  uint32_t base;
+  int slot = 0;                                          // of the warp's last tile
+  expert_plan_tiles<kExpertTileN>(sh.tiles, p, base);
   const int total = sh.tiles.first_tile[p.n_slots] * p.m_blocks;
   const int stride = static_cast<int>(gridDim.x) / 2, first = static_cast<int>(blockIdx.x) / 2;
-  const uint32_t base = p.slot_offsets != nullptr ? p.slot_offsets[0] : 0u;
   // Few rows per tile leave room for more stages: what is under way is W, and a launch of few tiles has few blocks to ask for it.
   const uint32_t stage_bytes = kExpertWBytes + 64u * static_cast<uint32_t>(max(sh.tiles.most, kExpertStepN));
   const uint32_t stages = min(kExpertRingBytes / stage_bytes, static_cast<uint32_t>(kExpertStages));
@@ -348,7 +394,7 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
     uint32_t s = 0, phase = 0, fills = 0;
     bool ok = true;
     for (int g = first; g < total && ok; g += stride) {
-      const ExpertTile t = expert_tile<kExpertTileN>(sh.tiles, p, g);
+      const ExpertTile t = expert_tile<kExpertTileN>(sh.tiles, p, g, slot);
       const int half = t.n / 2, x_row = t.row + rank * half + kTileLoadRows * lane;
       const uint32_t bytes = 2u * kExpertWBytes + (gather ? 0u : 128u * static_cast<uint32_t>(t.n));
       for (int kb = 0; kb < p.num_kb; ++kb) {
@@ -382,16 +428,12 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
     uint32_t s = 0, phase = 0, used = 0;                 // accumulators begun
     bool ok = true;
     for (int g = first; g < total && ok; g += stride) {
-      const ExpertTile t = expert_tile<kExpertTileN>(sh.tiles, p, g);
+      const ExpertTile t = expert_tile<kExpertTileN>(sh.tiles, p, g, slot);
       const uint32_t idesc = umma_idesc_bf16_f32(256, static_cast<uint32_t>(t.n)), a = used & 1u, acc = tmem + a * kExpertTileN;
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.acc_empty[a]), ((used >> 1) & 1u) ^ 1u, abort_flag));
       if (!ok) break;
       for (int kb = 0; kb < p.num_kb; ++kb) {
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.full_bar[s]), phase, abort_flag));
-        if (ok && gather) {
-          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.x_bar[s]), phase, abort_flag));
-          fence_proxy_async();
-        }
         if (!ok) break;
         tcgen05_fence_after();
         const uint32_t w_addr = smem + s * stage_bytes;
@@ -408,27 +450,16 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
       }
       ++used;
     }
-  } else if (warp == 1 && gather) {
-    // -------------------------------------------------------------- odd block: its gathered rows are there
-    uint32_t s = 0, phase = 0;
-    bool ok = true;
-    for (int g = first; g < total && ok; g += stride)
-      for (int kb = 0; kb < p.num_kb; ++kb) {
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.x_bar[s]), phase, abort_flag));
-        if (!ok) break;
-        fence_proxy_async();
-        if (lane == 0) mbar_arrive_pair(smem_u32(&sh.full_bar[s]), 0u);
-        __syncwarp();
-        if (++s == stages) { s = 0; phase ^= 1u; }
-      }
+  } else if (warp == 2 && gather) {
+    pass_on_rows(p, total, first, stride, stages, sh.x_bar, abort_flag, [&](uint32_t s) { mbar_arrive_pair(smem_u32(&sh.full_bar[s]), 0u); });
   } else if (warp >= kExpertFirstGatherWarp) {
     if (gather)
       gather_rows(p, total, first, stride, smem + kExpertWBytes, stages, stage_bytes, sh.empty_bar, sh.x_bar, abort_flag,
                                                     [&](int g, int row0, int32_t (&r)[kGatherRows]) {
-        const ExpertTile t = expert_tile<kExpertTileN>(sh.tiles, p, g);
+        const ExpertTile t = expert_tile<kExpertTileN>(sh.tiles, p, g, slot);
 #pragma unroll
         for (int i = 0; i < kGatherRows; ++i)
-          r[i] = 16 * i < t.n / 2 ? expert_x_row(p, base, t, rank * (t.n / 2) + row0 + 16 * i) : -1;
+          r[i] = 16 * i < t.n / 2 ? expert_x_row(p, base, t, rank * (t.n / 2) + row0 + 16 * i) : kNoRow;
       });
   } else if (warp >= kExpertFirstEpilogueWarp) {
     // -------------------------------------------------------------- results
@@ -442,7 +473,7 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
     uint32_t used = 0;
     bool ok = true;
     for (int g = first; g < total && ok; g += stride) {
-      const ExpertTile t = expert_tile<kExpertTileN>(sh.tiles, p, g);
+      const ExpertTile t = expert_tile<kExpertTileN>(sh.tiles, p, g, slot);
       const int column = (kSwiglu ? t.m * 128 + rank * 64 + quarter * 16 : t.m * 256 + rank * 128 + quarter * 32) + unit * 8;
       const uint32_t a = used & 1u;
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.acc_full[a]), (used >> 1) & 1u, abort_flag));

@@ -10,7 +10,7 @@
 // shared memory for every k-block; that, tcgen05.ld in its 16-lane form and the way over two blocks at each hand-over took
 // 880 cycles per k-block whose MMAs take 512.
 //
-// One block per SM.  Warps: 0 loads by TMA, 1 issues the MMAs, 4-11 add up and store, 12-15 gather rows of x.  Two
+// One block per SM.  Warps: 0 loads by TMA, 1 issues the MMAs, 2 passes on that gathered rows are there, 4-11 add up and store, 12-15 gather rows of x.  Two
 // accumulators of 256 columns: the MMAs fill one while the other is added up.
 #pragma once
 #include "fb_experts.cuh"
@@ -84,11 +84,10 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
 
   if (threadIdx.x == 0) {
     sh.abort_flag = 0;
-    sh.tiles.most = 0;
     for (int s = 0; s < kE4m3Stages; ++s) {
-      mbar_init(smem_u32(&sh.full_bar[s]), 1);
+      mbar_init(smem_u32(&sh.full_bar[s]), gather ? 2 : 1);        // the TMA loads; gathered rows
       mbar_init(smem_u32(&sh.empty_bar[s]), 1);
-      mbar_init(smem_u32(&sh.x_bar[s]), 32 * kGatherWarps);
+      mbar_init(smem_u32(&sh.x_bar[s]), 33 * kGatherWarps);
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(smem_u32(&sh.acc_full[a]), 1);
@@ -109,10 +108,11 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
   pdl_wait();
   pdl_launch_dependents();
   const uint32_t tmem = sh.tmem_base;
-  expert_plan_tiles<kE4m3Rows>(sh.tiles, p);
+  uint32_t base;
+  int slot = 0;                                          // of the warp's last tile
+  expert_plan_tiles<kE4m3Rows>(sh.tiles, p, base);
   const int total = sh.tiles.first_tile[p.n_slots] * p.m_blocks;
   const int stride = static_cast<int>(gridDim.x), first = static_cast<int>(blockIdx.x);
-  const uint32_t base = p.slot_offsets != nullptr ? p.slot_offsets[0] : 0u;
 
   // Registers: 256 threads with 208 and 256 with 48 are the 512 x 128 of the launch.
   if (warp < kExpertFirstEpilogueWarp) {
@@ -123,9 +123,11 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
       uint32_t s = 0, phase = 0, fills = 0;
       bool ok = true;
       for (int g = first; g < total && ok; g += stride) {
-        const ExpertTile t = expert_tile<kE4m3Rows>(sh.tiles, p, g);
-        const int x_loads = gather ? 0 : (t.valid + kTileLoadRows - 1) / kTileLoadRows;      // rows behind the tile's last hold what they held
-        const uint32_t bytes = kE4m3WBytes + 128u * kTileLoadRows * static_cast<uint32_t>(x_loads);
+        const ExpertTile t = expert_tile<kE4m3Rows>(sh.tiles, p, g, slot);
+        const int x_loads = gather ? 0 : kE4m3Rows / kTileLoadRows;
+        const uint32_t bytes = kE4m3WBytes + (gather ? 0u : kE4m3XBytes);
+        // (loads without a row of the tile begin behind the last row of x and give zeros)
+        const int x_row = kTileLoadRows * lane < t.valid ? t.row + kTileLoadRows * lane : p.x_rows;
         for (int kb = 0; kb < p.num_kb; ++kb) {
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.empty_bar[s]), phase ^ 1u, abort_flag));
           if (!ok) break;
@@ -136,7 +138,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
             else tma_load_3d(x_dst + kE4m3XBytes, &map_w, full, kb * 128, t.m * kExpertTileM, t.slot);
           }
           __syncwarp();
-          if (lane < x_loads) tma_load_rows(x_dst + 128u * kTileLoadRows * lane, &map_x, full, kb * 128, t.row + kTileLoadRows * lane);
+          if (lane < x_loads) tma_load_rows(x_dst + 128u * kTileLoadRows * lane, &map_x, full, kb * 128, x_row);
           __syncwarp();
           ++fills;
           if (++s == kE4m3Stages) { s = 0; phase ^= 1u; }
@@ -157,10 +159,6 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
         for (int kb = 0; kb < p.num_kb; ++kb) {
           const uint32_t a = used & 1u, acc = tmem + a * 256u;
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.full_bar[s]), phase, abort_flag));
-          if (ok && gather) {
-            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.x_bar[s]), phase, abort_flag));
-            fence_proxy_async();
-          }
           if (ok) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.acc_empty[a]), ((used >> 1) & 1u) ^ 1u, abort_flag));
           if (!ok) break;
           tcgen05_fence_after();
@@ -177,15 +175,17 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
           if (++s == kE4m3Stages) { s = 0; phase ^= 1u; }
         }
       }
+    } else if (warp == 2 && gather) {
+      pass_on_rows(p, total, first, stride, kE4m3Stages, sh.x_bar, abort_flag, [&](uint32_t s) { mbar_arrive(smem_u32(&sh.full_bar[s])); });
     }
   } else if (warp >= kExpertFirstGatherWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (gather)
       gather_rows(p, total, first, stride, smem, kE4m3Stages, kE4m3StageBytes, sh.empty_bar, sh.x_bar, abort_flag,
                                                 [&](int g, int row0, int32_t (&r)[kGatherRows]) {
-        const ExpertTile t = expert_tile<kE4m3Rows>(sh.tiles, p, g);
+        const ExpertTile t = expert_tile<kE4m3Rows>(sh.tiles, p, g, slot);
 #pragma unroll
-        for (int i = 0; i < kGatherRows; ++i) r[i] = row0 + 16 * i < t.valid ? expert_x_row(p, base, t, row0 + 16 * i) : -1;
+        for (int i = 0; i < kGatherRows; ++i) r[i] = expert_x_row(p, base, t, row0 + 16 * i);
       });
   } else {
     // -------------------------------------------------------------- sums and results
@@ -206,7 +206,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
       if constexpr (kSwiglu) a1[j] = w1[kb];
     };
     auto begin = [&](const ExpertTile& t) {
-      xs = p.x_scale + static_cast<size_t>(expert_x_row(p, base, t, row)) * p.scale_k;
+      xs = p.x_scale + static_cast<size_t>(max(expert_x_row(p, base, t, row), 0)) * p.scale_k;
       const float* ws = p.w_scale + static_cast<size_t>(t.slot) * p.w_scale_slot;
       const int blocks = (p.n_out + 127) / 128;          // (the second half of a tile may lie behind the last row of W: not stored)
       w0 = ws + static_cast<size_t>(kSwiglu ? t.m : min(2 * t.m + half, blocks - 1)) * p.scale_k;
@@ -230,16 +230,26 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
       }
       __syncwarp();
     };
+    auto release = [&](uint32_t a) {                     // this warp has read the accumulator
+      tcgen05_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sh.acc_empty[a]));
+    };
     ExpertTile t;
     if (first < total) {
-      t = expert_tile<kE4m3Rows>(sh.tiles, p, first);
+      t = expert_tile<kE4m3Rows>(sh.tiles, p, first, slot);
       begin(t);
     }
     for (int g = first; g < total && ok; g += stride) {
       float acc[128];                                    // SwiGLU: 16 gate, 16 up, ..
 #pragma unroll
       for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
-      for (int kb0 = 0; kb0 < p.num_kb && ok; kb0 += kE4m3Ahead) {
+      const bool any = quarter * 32 < t.valid;           // this warp has rows of x here
+      for (int kb = any ? p.num_kb : 0; kb < p.num_kb && ok; ++kb, ++used) {
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.acc_full[used & 1u]), (used >> 1) & 1u, abort_flag));
+        if (ok) release(used & 1u);
+      }
+      for (int kb0 = any ? 0 : p.num_kb; kb0 < p.num_kb && ok; kb0 += kE4m3Ahead) {
 #pragma unroll
         for (int j = 0; j < kE4m3Ahead; ++j) {
           if (kb0 + j >= p.num_kb || !ok) break;
@@ -249,30 +259,37 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.acc_full[a]), (used >> 1) & 1u, abort_flag));
           if (!ok) break;
           tcgen05_fence_after();
-          // 16 columns are added while the next 16 are on their way
-          uint32_t r[2][16];
-          tmem_ld_32x32b_x16(from + 256u * a, r[0]);
+          // 32 and 16 columns in turn are added while the next ones are on their way
+          uint32_t wide[32], narrow[16];
+          auto add = [&](int c, const uint32_t* r, int n) {
 #pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            tmem_ld_wait();
-            if (c < 7) {
-              tmem_ld_32x32b_x16(from + 256u * a + 16u * (c + 1), r[(c + 1) & 1]);
-            } else {
-              tcgen05_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(smem_u32(&sh.acc_empty[a]));
-            }
-#pragma unroll
-            for (int i = 0; i < 16; i += 2)
-              fma_two(acc[16 * c + i], acc[16 * c + i + 1], r[c & 1][i], r[c & 1][i + 1], (c & 1) == 0 ? s0 : s1);
-          }
+            for (int i = 0; i < 32; i += 2)
+              if (i < n) fma_two(acc[c + i], acc[c + i + 1], r[i], r[i + 1], ((c + i) & 16) == 0 ? s0 : s1);
+          };
+          const uint32_t at = from + 256u * a;
+          tmem_ld_32x32b_x32(at, wide);
+          tmem_ld_wait();
+          tmem_ld_32x32b_x16(at + 32u, narrow);
+          add(0, wide, 32);
+          tmem_ld_wait();
+          tmem_ld_32x32b_x32(at + 48u, wide);
+          add(32, narrow, 16);
+          tmem_ld_wait();
+          tmem_ld_32x32b_x16(at + 80u, narrow);
+          add(48, wide, 32);
+          tmem_ld_wait();
+          tmem_ld_32x32b_x32(at + 96u, wide);
+          add(80, narrow, 16);
+          tmem_ld_wait();
+          release(a);
+          add(96, wide, 32);
           ++used;
         }
       }
       if (!ok) break;
       const ExpertTile done = t;
       if (g + stride < total) {                          // the next tile's first scales arrive under the stores
-        t = expert_tile<kE4m3Rows>(sh.tiles, p, g + stride);
+        t = expert_tile<kE4m3Rows>(sh.tiles, p, g + stride, slot);
         begin(t);
       }
       if constexpr (kSwiglu) {
