@@ -21,6 +21,9 @@
 #include "fb_router_persistent.cuh"
 #include "fb_router_rows.cuh"
 
+#ifndef E4M3_PAIR
+#define E4M3_PAIR (rows / m->n_slots >= 256)
+#endif
 namespace {
 
 using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
@@ -516,14 +519,17 @@ struct ExpertKernel {
   ExpertKernelFn fn;
   size_t smem;
 };
-ExpertKernel expert_kernel(bool e4m3, bool swiglu, bool quantize) {
-  if (!e4m3) {
-    if (swiglu) return {fb::fb_expert_matmul_kernel<true>, fb::ExpertLayout<true>::kDynamic};
-    return {fb::fb_expert_matmul_kernel<false>, fb::ExpertLayout<false>::kDynamic};
-  }
-  if (!swiglu) return {fb::fb_expert_matmul_e4m3_kernel<false, false>, fb::kE4m3Dynamic};
-  if (!quantize) return {fb::fb_expert_matmul_e4m3_kernel<true, false>, fb::kE4m3Dynamic};
-  return {fb::fb_expert_matmul_e4m3_kernel<true, true>, fb::kE4m3Dynamic};
+template <bool kPair>
+ExpertKernel e4m3_kernel(bool swiglu, bool quantize) {
+  constexpr size_t kSmem = fb::ExpertE4m3Layout<kPair>::kDynamic;
+  if (!swiglu) return {fb::fb_expert_matmul_e4m3_kernel<kPair, false, false>, kSmem};
+  if (!quantize) return {fb::fb_expert_matmul_e4m3_kernel<kPair, true, false>, kSmem};
+  return {fb::fb_expert_matmul_e4m3_kernel<kPair, true, true>, kSmem};
+}
+ExpertKernel expert_kernel(bool e4m3, bool pair, bool swiglu, bool quantize) {
+  if (e4m3) return pair ? e4m3_kernel<true>(swiglu, quantize) : e4m3_kernel<false>(swiglu, quantize);
+  if (swiglu) return {fb::fb_expert_matmul_kernel<true>, fb::ExpertLayout<true>::kDynamic};
+  return {fb::fb_expert_matmul_kernel<false>, fb::ExpertLayout<false>::kDynamic};
 }
 
 // A fixed one-swap plan over two slots for fb_calibrate_exchange: [placement: 2][swap: 4][n: 1].
@@ -659,7 +665,8 @@ static fb_status set_up_device(fb_ctx* ctx, int device, const DeviceLimits& dev)
   const int plan_general = raise(reinterpret_cast<const void*>(fb::fb_plan_kernel<true>));
   const int plan_uniform = raise(reinterpret_cast<const void*>(fb::fb_plan_kernel<false>));
   ctx->own_sm.smem = plan_general < plan_uniform ? plan_general : plan_uniform;
-  for (int i = 0; i < 5; ++i) raise(reinterpret_cast<const void*>(expert_kernel(i >= 2, i == 1 || i >= 3, i == 4).fn));
+  for (int i = 0; i < 8; ++i)                             // bf16; e4m3 single, pair: without SwiGLU, with it, quantised
+    raise(reinterpret_cast<const void*>((i < 2 ? expert_kernel(false, true, i == 1, false) : expert_kernel(true, i >= 5, (i - 2) % 3 != 0, (i - 2) % 3 == 2)).fn));
   int least = 0;
   ok = ok && cudaDeviceGetStreamPriorityRange(&least, &ctx->own_sm.priority) == cudaSuccess;
   if (!ok) { cudaGetLastError(); return FB_ERR_CUDA; }
@@ -1196,8 +1203,9 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   p.n_out = swiglu ? m->n / 2 : m->n;
   p.m_blocks = (m->n + fb::kExpertTileM - 1) / fb::kExpertTileM;
   p.scale_k = (m->K + 127) / 128;
+  const bool pair = !e4m3 || E4M3_PAIR;
   // a slot of c rows has at most ceil(c / tile) tiles of rows
-  const int64_t tiles = (rows / (e4m3 ? fb::kE4m3Rows : fb::kExpertTileN) + (m->n_slots < rows ? m->n_slots : rows)) * static_cast<int64_t>(p.m_blocks);
+  const int64_t tiles = (rows / (pair ? 256 : 128) + (m->n_slots < rows ? m->n_slots : rows)) * static_cast<int64_t>(p.m_blocks);
   if (tiles >= (int64_t{1} << 31)) return FB_ERR_UNSUPPORTED_SHAPE;
   CUtensorMap map_x, map_w;
   const CUtensorMapDataType type = e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
@@ -1220,21 +1228,21 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   if (swiglu) {                                                    // 16 rows of gate, 16 of up, ..
     const cuuint64_t size[5] = {K, 16, 2, static_cast<cuuint64_t>(p.n_out / 16), E};
     const cuuint64_t stride[4] = {row_bytes, row_bytes * p.n_out, row_bytes * 16, slot_bytes};
-    const cuuint32_t box[5] = {width, 16, 2, e4m3 ? 8u : 4u, 1};
+    const cuuint32_t box[5] = {width, 16, 2, pair ? 4u : 8u, 1};
     ok = ok && encode(&map_w, 5, m->w, size, stride, box);
   } else {
     const cuuint64_t size[3] = {K, static_cast<cuuint64_t>(m->n), E}, stride[2] = {row_bytes, slot_bytes};
-    const cuuint32_t box[3] = {width, e4m3 ? 256u : 128u, 1};
+    const cuuint32_t box[3] = {width, pair ? 128u : 256u, 1};
     ok = ok && encode(&map_w, 3, m->w, size, stride, box);
   }
   if (!ok) return FB_ERR_CUDA;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return FB_ERR_CUDA;
-  const ExpertKernel kernel = expert_kernel(e4m3, swiglu, out_scale != nullptr);
-  const int64_t at_once = e4m3 ? ctx->n_sm : ctx->max_clusters[1], workers = tiles < at_once ? tiles : at_once;      // blocks, or pairs of them
+  const ExpertKernel kernel = expert_kernel(e4m3, pair, swiglu, out_scale != nullptr);
+  const int64_t at_once = pair ? ctx->max_clusters[1] : ctx->n_sm, workers = tiles < at_once ? tiles : at_once;      // blocks, or pairs of them
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3(static_cast<unsigned>(e4m3 ? workers : 2 * workers), 1, 1);
+  cfg.gridDim = dim3(static_cast<unsigned>(pair ? 2 * workers : workers), 1, 1);
   cfg.blockDim = dim3(fb::kExpertThreads, 1, 1);
   cfg.dynamicSmemBytes = kernel.smem;
   cfg.stream = static_cast<cudaStream_t>(stream_);
@@ -1246,7 +1254,7 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = e4m3 ? 1 : 2;
+  cfg.numAttrs = pair ? 2 : 1;
   const cudaError_t err = launch_refused(ctx) ? cudaErrorUnknown : cudaLaunchKernelEx(&cfg, kernel.fn, map_x, map_w, p);
   return err == cudaSuccess ? FB_OK : FB_ERR_CUDA;
 }

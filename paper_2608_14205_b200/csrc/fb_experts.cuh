@@ -378,7 +378,7 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
   tcgen05_fence_after();
   pdl_wait();
   pdl_launch_dependents();
-  const uint32_t tmem = sh.tmem_base;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem_base, 0);      // (warp-uniform for the compiler as well)
   uint32_t base;
   int slot = 0;                                          // of the warp's last tile
   expert_plan_tiles<kExpertTileN>(sh.tiles, p, base);

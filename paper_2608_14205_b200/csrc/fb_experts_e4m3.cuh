@@ -10,6 +10,10 @@
 // shared memory for every k-block; that, tcgen05.ld in its 16-lane form and the way over two blocks at each hand-over took
 // 880 cycles per k-block whose MMAs take 512.
 //
+// kPair: two blocks (cta_group::2) take 256 rows of x by 256 of W, each with its 128 rows of x and half of the rows of W
+// in its shared memory; else one block takes 128 x 256.  The pair brings 32 KB into an SM per k-block, the single block
+// 48 KB; the single block's tiles fit counts better that are no multiple of 256 (the rule is in fb_expert_matmul).
+//
 // One block per SM.  Warps: 0 loads by TMA, 1 issues the MMAs, 2 passes on that gathered rows are there, 4-11 add up and store, 12-15 gather rows of x.  Two
 // accumulators of 256 columns: the MMAs fill one while the other is added up.
 #pragma once
@@ -17,21 +21,26 @@
 
 namespace fb {
 
-constexpr int kE4m3Stages = 4;
-constexpr int kE4m3Rows = 128;                          // of x per tile
-constexpr uint32_t kE4m3XBytes = 128 * 128, kE4m3WBytes = 256 * 128, kE4m3StageBytes = kE4m3XBytes + kE4m3WBytes;
-constexpr int kE4m3Ahead = 4;                           // k-blocks whose scales are on their way
+constexpr uint32_t kE4m3XBytes = 128 * 128;             // a block's rows of x in a stage
 constexpr uint32_t kE4m3WarpStaging = 32 * 64;          // 32 rows of 64 bytes
-constexpr uint32_t kE4m3StagingAt = kE4m3Stages * kE4m3StageBytes;
-constexpr uint32_t kE4m3Dynamic = kE4m3StagingAt + kExpertEpilogueWarps * kE4m3WarpStaging + 1024;
+template <bool kPair>
+struct ExpertE4m3Layout {
+  static constexpr int kRows = kPair ? 256 : 128;       // of x per tile
+  static constexpr int kStages = kPair ? 6 : 4;
+  static constexpr uint32_t kWBytes = (kPair ? 128 : 256) * 128;        // a block's rows of W in a stage
+  static constexpr uint32_t kStageBytes = kE4m3XBytes + kWBytes;
+  static constexpr uint32_t kStagingAt = kStages * kStageBytes;
+  static constexpr uint32_t kDynamic = kStagingAt + kExpertEpilogueWarps * kE4m3WarpStaging + 1024;
+};
+constexpr int kE4m3Ahead = 4;                           // k-blocks whose scales are on their way
 
 struct ExpertE4m3Shared {
-  uint64_t full_bar[kE4m3Stages], empty_bar[kE4m3Stages], x_bar[kE4m3Stages];
+  uint64_t full_bar[6], empty_bar[6], x_bar[6];
   uint64_t acc_full[2], acc_empty[2];
   uint64_t top_bar[4];                                  // per quarter: its two warps' maxima are there
   uint32_t tmem_base;
   int32_t abort_flag;
-  float top[2][2][kE4m3Rows];                           // in turn; per half of the columns: a row's largest output
+  float top[2][2][128];                                 // in turn; per half of the columns: a row's largest output
   ExpertTiles tiles;
 };
 
@@ -53,12 +62,20 @@ __device__ __forceinline__ void tma_load_5d(uint32_t dst, const void* tmap, uint
 }
 // e4m3 x e4m3 -> fp32, both operands K-major.
 __device__ __forceinline__ uint32_t umma_idesc_e4m3_f32(uint32_t M, uint32_t N) { return (1u << 4) | ((N >> 3) << 17) | ((M >> 4) << 24); }
+template <int kCtaGroup>
 __device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(tmem_d),
-      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
-      : "memory");
+  if constexpr (kCtaGroup == 1)
+    asm volatile(
+        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(tmem_d),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(tmem_d),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
 }
 __device__ __forceinline__ void umma_commit_one(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -70,28 +87,31 @@ __device__ __forceinline__ void fma_two(float& d0, float& d1, uint32_t a0, uint3
       : "+f"(d0), "+f"(d1)
       : "r"(a0), "r"(a1), "f"(s));
 }
-template <bool kSwiglu, bool kQuantize>
+template <bool kPair, bool kSwiglu, bool kQuantize>
 __global__ void __launch_bounds__(kExpertThreads, 1)
 fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                              const __grid_constant__ ExpertParams p) {
+  using L = ExpertE4m3Layout<kPair>;
+  constexpr int kGroup = kPair ? 2 : 1;                  // blocks per tile
   extern __shared__ uint8_t smem_raw[];
   __shared__ ExpertE4m3Shared sh;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
   const int lane = threadIdx.x & 31;
+  const int rank = kPair ? static_cast<int>(cluster_ctarank()) : 0;
   const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
   volatile int* abort_flag = &sh.abort_flag;
   const bool gather = p.perm != nullptr;
 
   if (threadIdx.x == 0) {
     sh.abort_flag = 0;
-    for (int s = 0; s < kE4m3Stages; ++s) {
-      mbar_init(smem_u32(&sh.full_bar[s]), gather ? 2 : 1);        // the TMA loads; gathered rows
+    for (int s = 0; s < L::kStages; ++s) {
+      mbar_init(smem_u32(&sh.full_bar[s]), gather ? 1 + kGroup : 1);    // the TMA loads; each block's gathered rows
       mbar_init(smem_u32(&sh.empty_bar[s]), 1);
       mbar_init(smem_u32(&sh.x_bar[s]), 33 * kGatherWarps);
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(smem_u32(&sh.acc_full[a]), 1);
-      mbar_init(smem_u32(&sh.acc_empty[a]), kExpertEpilogueWarps);
+      mbar_init(smem_u32(&sh.acc_empty[a]), kGroup * kExpertEpilogueWarps);
     }
     for (int q = 0; q < 4; ++q) mbar_init(smem_u32(&sh.top_bar[q]), 2);
     fence_mbar_init();
@@ -99,20 +119,21 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
     prefetch_tensormap(&map_w);
   }
   if (warp == 1) {
-    tmem_alloc<1>(smem_u32(&sh.tmem_base), 512);
-    tmem_relinquish<1>();
+    tmem_alloc<kGroup>(smem_u32(&sh.tmem_base), 512);
+    tmem_relinquish<kGroup>();
   }
   tcgen05_fence_before();
   __syncthreads();
+  if constexpr (kPair) { cluster_arrive_relaxed(); cluster_wait(); }      // the partner's barriers and tensor memory are ready too
   tcgen05_fence_after();
   pdl_wait();
   pdl_launch_dependents();
-  const uint32_t tmem = sh.tmem_base;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem_base, 0);      // (warp-uniform for the compiler as well)
   uint32_t base;
   int slot = 0;                                          // of the warp's last tile
-  expert_plan_tiles<kE4m3Rows>(sh.tiles, p, base);
+  expert_plan_tiles<L::kRows>(sh.tiles, p, base);
   const int total = sh.tiles.first_tile[p.n_slots] * p.m_blocks;
-  const int stride = static_cast<int>(gridDim.x), first = static_cast<int>(blockIdx.x);
+  const int stride = static_cast<int>(gridDim.x) / kGroup, first = static_cast<int>(blockIdx.x) / kGroup;
 
   // Registers: 256 threads with 208 and 256 with 48 are the 512 x 128 of the launch.
   if (warp < kExpertFirstEpilogueWarp) {
@@ -123,36 +144,46 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
       uint32_t s = 0, phase = 0, fills = 0;
       bool ok = true;
       for (int g = first; g < total && ok; g += stride) {
-        const ExpertTile t = expert_tile<kE4m3Rows>(sh.tiles, p, g, slot);
-        const int x_loads = gather ? 0 : kE4m3Rows / kTileLoadRows;
-        const uint32_t bytes = kE4m3WBytes + (gather ? 0u : kE4m3XBytes);
+        const ExpertTile t = expert_tile<L::kRows>(sh.tiles, p, g, slot);
         // (loads without a row of the tile begin behind the last row of x and give zeros)
-        const int x_row = kTileLoadRows * lane < t.valid ? t.row + kTileLoadRows * lane : p.x_rows;
+        const int i = rank * 128 + kTileLoadRows * lane, x_row = i < t.valid ? t.row + i : p.x_rows;
+        const uint32_t bytes = kGroup * (L::kWBytes + (gather ? 0u : kE4m3XBytes));
         for (int kb = 0; kb < p.num_kb; ++kb) {
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.empty_bar[s]), phase ^ 1u, abort_flag));
           if (!ok) break;
-          const uint32_t x_dst = smem + s * kE4m3StageBytes, full = smem_u32(&sh.full_bar[s]);
+          const uint32_t x_dst = smem + s * L::kStageBytes, w_dst = x_dst + kE4m3XBytes;
+          const uint32_t full = kPair ? map_to_cta(smem_u32(&sh.full_bar[s]), 0u) : smem_u32(&sh.full_bar[s]);
           if (leader) {
-            mbar_arrive_expect_tx(full, bytes);
-            if constexpr (kSwiglu) tma_load_5d(x_dst + kE4m3XBytes, &map_w, full, kb * 128, 0, 0, t.m * (kExpertTileM / 2) / 16, t.slot);
-            else tma_load_3d(x_dst + kE4m3XBytes, &map_w, full, kb * 128, t.m * kExpertTileM, t.slot);
+            if (rank == 0) mbar_arrive_expect_tx(smem_u32(&sh.full_bar[s]), bytes);
+            if constexpr (kSwiglu) {
+              const int w_group = t.m * (kExpertTileM / 2 / 16) + rank * 4;      // of 16 outputs
+              if constexpr (kPair) tma_load_5d_pair(w_dst, &map_w, full, kb * 128, 0, 0, w_group, t.slot);
+              else tma_load_5d(w_dst, &map_w, full, kb * 128, 0, 0, w_group, t.slot);
+            } else {
+              const int w_row = t.m * kExpertTileM + rank * 128;
+              if constexpr (kPair) tma_load_3d_pair(w_dst, &map_w, full, kb * 128, w_row, t.slot);
+              else tma_load_3d(w_dst, &map_w, full, kb * 128, w_row, t.slot);
+            }
           }
           __syncwarp();
-          if (lane < x_loads) tma_load_rows(x_dst + 128u * kTileLoadRows * lane, &map_x, full, kb * 128, x_row);
+          if (!gather && lane < 128 / kTileLoadRows) {
+            if constexpr (kPair) tma_load_rows_pair(x_dst + 128u * kTileLoadRows * lane, &map_x, full, kb * 128, x_row);
+            else tma_load_rows(x_dst + 128u * kTileLoadRows * lane, &map_x, full, kb * 128, x_row);
+          }
           __syncwarp();
           ++fills;
-          if (++s == kE4m3Stages) { s = 0; phase ^= 1u; }
+          if (++s == L::kStages) { s = 0; phase ^= 1u; }
         }
       }
-      if (!ok) {                                         // given up: the copies under way end before the block does
+      if (!ok && rank == 0) {                            // given up: the copies under way end before the block does
         volatile int never = 0;
-        for (uint32_t f = fills > kE4m3Stages ? fills - kE4m3Stages : 0; f < fills; ++f)
-          mbar_wait(smem_u32(&sh.full_bar[f % kE4m3Stages]), (f / kE4m3Stages) & 1u, &never);
+        for (uint32_t f = fills > L::kStages ? fills - L::kStages : 0; f < fills; ++f)
+          mbar_wait(smem_u32(&sh.full_bar[f % L::kStages]), (f / L::kStages) & 1u, &never);
       }
-    } else if (warp == 1) {
+    } else if (warp == 1 && rank == 0) {
       // ------------------------------------------------------------ MMAs
       const bool leader = elect_one();
-      const uint32_t idesc = umma_idesc_e4m3_f32(128, 256);
+      const uint32_t idesc = umma_idesc_e4m3_f32(128 * kGroup, 256);
       uint32_t s = 0, phase = 0, used = 0;               // accumulators begun
       bool ok = true;
       for (int g = first; g < total && ok; g += stride) {
@@ -162,38 +193,46 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
           if (ok) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.acc_empty[a]), ((used >> 1) & 1u) ^ 1u, abort_flag));
           if (!ok) break;
           tcgen05_fence_after();
-          const uint32_t x_addr = smem + s * kE4m3StageBytes;
+          const uint32_t x_addr = smem + s * L::kStageBytes;
           const uint64_t adesc = umma_smem_desc_sw128(x_addr), bdesc = umma_smem_desc_sw128(x_addr + kE4m3XBytes);
           if (leader) {
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) umma_e4m3(acc, adesc + 2u * kk, bdesc + 2u * kk, idesc, kk != 0 ? 1u : 0u);      // 32 of K each
-            umma_commit_one(smem_u32(&sh.acc_full[a]));
-            umma_commit_one(smem_u32(&sh.empty_bar[s]));
+            for (int kk = 0; kk < 4; ++kk) umma_e4m3<kGroup>(acc, adesc + 2u * kk, bdesc + 2u * kk, idesc, kk != 0 ? 1u : 0u);      // 32 of K each
+            if constexpr (kPair) {
+              umma_commit_pair(smem_u32(&sh.acc_full[a]), 0u);
+              umma_commit_pair(smem_u32(&sh.empty_bar[s]), 0u);
+            } else {
+              umma_commit_one(smem_u32(&sh.acc_full[a]));
+              umma_commit_one(smem_u32(&sh.empty_bar[s]));
+            }
           }
           __syncwarp();
           ++used;
-          if (++s == kE4m3Stages) { s = 0; phase ^= 1u; }
+          if (++s == L::kStages) { s = 0; phase ^= 1u; }
         }
       }
     } else if (warp == 2 && gather) {
-      pass_on_rows(p, total, first, stride, kE4m3Stages, sh.x_bar, abort_flag, [&](uint32_t s) { mbar_arrive(smem_u32(&sh.full_bar[s])); });
+      pass_on_rows(p, total, first, stride, L::kStages, sh.x_bar, abort_flag, [&](uint32_t s) {
+        if constexpr (kPair) mbar_arrive_pair(smem_u32(&sh.full_bar[s]), 0u);
+        else mbar_arrive(smem_u32(&sh.full_bar[s]));
+      });
     }
   } else if (warp >= kExpertFirstGatherWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (gather)
-      gather_rows(p, total, first, stride, smem, kE4m3Stages, kE4m3StageBytes, sh.empty_bar, sh.x_bar, abort_flag,
+      gather_rows(p, total, first, stride, smem, L::kStages, L::kStageBytes, sh.empty_bar, sh.x_bar, abort_flag,
                                                 [&](int g, int row0, int32_t (&r)[kGatherRows]) {
-        const ExpertTile t = expert_tile<kE4m3Rows>(sh.tiles, p, g, slot);
+        const ExpertTile t = expert_tile<L::kRows>(sh.tiles, p, g, slot);
 #pragma unroll
-        for (int i = 0; i < kGatherRows; ++i) r[i] = expert_x_row(p, base, t, row0 + 16 * i);
+        for (int i = 0; i < kGatherRows; ++i) r[i] = expert_x_row(p, base, t, rank * 128 + row0 + 16 * i);
       });
   } else {
     // -------------------------------------------------------------- sums and results
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int quarter = warp & 3, half = (warp - kExpertFirstEpilogueWarp) >> 2;     // TMEM lanes (rows of x); 128 columns each
-    const int row = quarter * 32 + lane;                 // of the tile
+    const int row0 = rank * 128 + quarter * 32, row = row0 + lane;      // of the tile
     const uint32_t from = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + 128u * half;
-    const uint32_t staging = smem + kE4m3StagingAt + static_cast<uint32_t>(warp - kExpertFirstEpilogueWarp) * kE4m3WarpStaging;
+    const uint32_t staging = smem + L::kStagingAt + static_cast<uint32_t>(warp - kExpertFirstEpilogueWarp) * kE4m3WarpStaging;
     uint32_t used = 0, tiles_done = 0;
     bool ok = true;
     // scales of the next k-blocks: this thread's row, and the blocks of W (gate and up; or this half's)
@@ -225,26 +264,29 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
       for (int i = 0; i < 4; ++i) {
         const int r = 8 * i + (lane >> 2), unit = lane & 3;
         const uint4 w = ld_shared_v4(staging + static_cast<uint32_t>(r * 64 + ((unit ^ ((r >> 1) & 3)) << 4)));
-        if (quarter * 32 + r < t.valid && first_byte + 16 * unit < row_bytes)
-          *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.out) + static_cast<size_t>(t.row + quarter * 32 + r) * row_bytes + first_byte + 16 * unit) = w;
+        if (row0 + r < t.valid && first_byte + 16 * unit < row_bytes)
+          *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.out) + static_cast<size_t>(t.row + row0 + r) * row_bytes + first_byte + 16 * unit) = w;
       }
       __syncwarp();
     };
     auto release = [&](uint32_t a) {                     // this warp has read the accumulator
       tcgen05_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&sh.acc_empty[a]));
+      if (lane == 0) {
+        if constexpr (kPair) mbar_arrive_pair(smem_u32(&sh.acc_empty[a]), 0u);
+        else mbar_arrive(smem_u32(&sh.acc_empty[a]));
+      }
     };
     ExpertTile t;
     if (first < total) {
-      t = expert_tile<kE4m3Rows>(sh.tiles, p, first, slot);
+      t = expert_tile<L::kRows>(sh.tiles, p, first, slot);
       begin(t);
     }
     for (int g = first; g < total && ok; g += stride) {
       float acc[128];                                    // SwiGLU: 16 gate, 16 up, ..
 #pragma unroll
       for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
-      const bool any = quarter * 32 < t.valid;           // this warp has rows of x here
+      const bool any = row0 < t.valid;           // this warp has rows of x here
       for (int kb = any ? p.num_kb : 0; kb < p.num_kb && ok; ++kb, ++used) {
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.acc_full[used & 1u]), (used >> 1) & 1u, abort_flag));
         if (ok) release(used & 1u);
@@ -289,7 +331,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
       if (!ok) break;
       const ExpertTile done = t;
       if (g + stride < total) {                          // the next tile's first scales arrive under the stores
-        t = expert_tile<kE4m3Rows>(sh.tiles, p, g + stride, slot);
+        t = expert_tile<L::kRows>(sh.tiles, p, g + stride, slot);
         begin(t);
       }
       if constexpr (kSwiglu) {
@@ -313,13 +355,13 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
         float top = 0x1p-100f;                           // smallest scale: see fb_quantize_rows
 #pragma unroll
         for (int i = 0; i < 64; ++i) top = fmaxf(top, fabsf(acc[i]));
-        float (&tops)[2][kE4m3Rows] = sh.top[tiles_done & 1u];
-        tops[half][row] = top;
+        float (&tops)[2][128] = sh.top[tiles_done & 1u];
+        tops[half][quarter * 32 + lane] = top;
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sh.top_bar[quarter]));
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.top_bar[quarter]), tiles_done & 1u, abort_flag));
         if (!ok) break;
-        top = fmaxf(top, tops[half ^ 1][row]);
+        top = fmaxf(top, tops[half ^ 1][quarter * 32 + lane]);
         const float inv = 448.0f / top;
         if (half == 0 && row < done.valid) p.out_scale[static_cast<size_t>(done.row + row) * ((p.n_out + 127) / 128) + done.m] = top / 448.0f;
 #pragma unroll
@@ -333,10 +375,11 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
   // ---------------------------------------------------------------- teardown
   tcgen05_fence_before();
   __syncthreads();
+  if constexpr (kPair) { cluster_arrive(); cluster_wait(); }              // nobody leaves while the partner may still signal it
   if (threadIdx.x == 0 && sh.abort_flag) atomicCAS(p.status, 0, FB_ERR_TIMEOUT);
   if (warp == 1) {
     tcgen05_fence_after();
-    tmem_dealloc<1>(tmem, 512);
+    tmem_dealloc<kGroup>(tmem, 512);
   }
 }
 
