@@ -21,9 +21,6 @@
 #include "fb_router_persistent.cuh"
 #include "fb_router_rows.cuh"
 
-#ifndef E4M3_PAIR
-#define E4M3_PAIR (rows / m->n_slots >= 256)
-#endif
 namespace {
 
 using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
@@ -1203,7 +1200,10 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   p.n_out = swiglu ? m->n / 2 : m->n;
   p.m_blocks = (m->n + fb::kExpertTileM - 1) / fb::kExpertTileM;
   p.scale_k = (m->K + 127) / 128;
-  const bool pair = !e4m3 || E4M3_PAIR;
+  // e4m3: tiles of 256 rows of x by pairs of blocks where the slots have 1024 rows and more on average, else of 128.  Under the
+  // power limit (single, pair; SwiGLU with quantised rows, K = n = 4096): 512 rows a slot, 256 slots of 7168 x 2048, 4908 and
+  // 5046 us; 1024 rows 1385 and 1363; 2048 rows 670 and 648; 8192 rows of one 8192 x 8192 matrix 565 and 530.
+  const bool pair = !e4m3 || rows / m->n_slots >= 1024;
   // a slot of c rows has at most ceil(c / tile) tiles of rows
   const int64_t tiles = (rows / (pair ? 256 : 128) + (m->n_slots < rows ? m->n_slots : rows)) * static_cast<int64_t>(p.m_blocks);
   if (tiles >= (int64_t{1} << 31)) return FB_ERR_UNSUPPORTED_SHAPE;

@@ -65,6 +65,9 @@ class Workload:
     fs_per_byte: int = 0
     expert_bytes: int = 0
     ranks_per_node: int = 0      # 0 -> all ranks in one node
+    # an expert's sizes: three matrices of d x inter (0: not given), bf16 or e4m3 with block scales
+    inter: int = 0
+    expert_e4m3: bool = False
 
     @property
     def m(self) -> int:
@@ -77,10 +80,10 @@ WORKLOADS = {
     "mixtral": Workload("mixtral", T=4096, d=4096, E=8, k=2, R=8, layers=32, rho=0.1,
                         skew="zipf", zipf_s=1.2, max_swaps=1),
     "qwen3": Workload("qwen3", T=8192, d=2048, E=128, k=8, R=8, layers=48, rho=0.15,
-                      skew="zipf", zipf_s=1.0, max_swaps=6, expert_bytes=9 * 2**20),
+                      skew="zipf", zipf_s=1.0, max_swaps=6, expert_bytes=9 * 2**20, inter=768),
     # The same model at the batch the paper evaluates it on: 16 sequences of 8K tokens.
     "qwen3_b16": Workload("qwen3_b16", T=131072, d=2048, E=128, k=8, R=8, layers=48, rho=0.15,
-                          skew="zipf", zipf_s=1.0, max_swaps=6, expert_bytes=9 * 2**20),
+                          skew="zipf", zipf_s=1.0, max_swaps=6, expert_bytes=9 * 2**20, inter=768),
     # Budget from the cost model: a 0.5 ms window, 44 MB per expert, 900 GB/s
     # (1111 fs per byte) and 2 us of fixed overhead give 99 858 ns per swap, so
     # exactly five swaps fit.
@@ -88,7 +91,8 @@ WORKLOADS = {
                      gate=GATE_SIGMOID_GROUP_TOPK, n_group=8, topk_group=4,
                      skew="clusters", zipf_s=1.1, n_clusters=3, max_swaps=128,
                      global_ns=500_000, rank_ns=500_000, link_ns=500_000,
-                     alpha_ns=2000, fs_per_byte=1111, expert_bytes=44_040_192),
+                     alpha_ns=2000, fs_per_byte=1111, expert_bytes=44_040_192, inter=2048,
+                     expert_e4m3=True),
     "sweep32k": Workload("sweep32k", T=32768, d=7168, E=256, k=8, R=64, layers=58, rho=0.2,
                          gate=GATE_SIGMOID_GROUP_TOPK, n_group=8, topk_group=4,
                          skew="clusters", zipf_s=1.1, n_clusters=3, max_swaps=5),

@@ -10,7 +10,8 @@ also dumps both passes' logits and the early ids, and the paper's prediction-qua
 
     python -m paper_2608_14205_b200.serving --workload dsv3 --steps 4 --layers 2
 
-prints one JSON report per run (synthetic changing-task steps, see inputs.make_step_layer).
+prints one JSON report per run (synthetic changing-task steps, see inputs.make_step_layer).  With ``--experts`` every
+layer also moves its experts' weights as planned and computes its output (random weights of the workload's sizes).
 """
 from __future__ import annotations
 
@@ -21,6 +22,7 @@ from typing import Dict, Optional
 import torch
 
 from . import binding as B
+from . import experts as X
 from . import inputs as I
 
 
@@ -53,6 +55,7 @@ class ServingLoop:
         self.placement: Dict[int, torch.Tensor] = {}      # layer -> expert_to_slot in force
         self._spare = i32(E)                              # receives the next placement
         self._q: Optional[dict] = None                    # quality-mode buffers, allocated on first use
+        self._x: Optional[X.ExpertBuffers] = None         # buffers of experts_step, allocated on first use
 
     def close(self):
         self.ctx.close()
@@ -108,6 +111,24 @@ class ServingLoop:
         self.placement[layer], self._spare = pi_new, pi
         return dict(out=o, pi_old=pi, pi_new=pi_new, **report)
 
+    def experts_step(self, r: dict, H: torch.Tensor, experts: X.SlotExperts, addend: Optional[torch.Tensor] = None,
+                     stream=None) -> torch.Tensor:
+        """The output of the layer whose step `r` layer_step returned last: [T, d], overwritten by the next call.
+
+        `experts` are the layer's images in the slots of the placement before that step; the plan's swaps are applied to
+        them first (stage 3 of the method), so the images are those of r["pi_new"] afterwards.  A step's swaps are
+        applied once: call this once per layer_step.  addend [T, d]: a shared expert's output or a residual."""
+        if torch._C._cuda_getDevice() != self.device:
+            with torch.cuda.device(self.device):
+                return self.experts_step(r, H, experts, addend, stream)
+        T, o, k = H.shape[0], self.out, self.wl.k
+        buf = self._x
+        if buf is None or buf.key != (experts.d, experts.inter, experts.e4m3, self.T_max, k):
+            buf = self._x = X.ExpertBuffers(experts, self.T_max, k)
+        experts.apply_swaps(r["pi_old"], o["swaps"], o["n_swaps"], o["swaps"].numel() // 4, stream=stream)
+        return X.run_experts(self.ctx, experts, buf, H, T, k, o["w"], o["slot_offsets"], o["perm"], o["inv_perm"], addend,
+                             stream)
+
     def realised_loads(self, r: dict, budget: B.FbBudget):
         """Realised per-expert counts of the last layer step and the rank loads they give under the
         old, the new and the identity placement - all from the library: per-slot counts of the
@@ -138,6 +159,16 @@ def max_over_mean(loads) -> float:
     return max(L) * len(L) / s if s else 1.0
 
 
+def random_experts(wl: I.Workload, layer: int, seed: int, dev: torch.device) -> X.SlotExperts:
+    """Images of random experts of the workload's sizes, expert e in slot e."""
+    x = X.SlotExperts(wl.E, wl.d, wl.inter, wl.expert_e4m3, dev.index or 0)
+    g = torch.Generator(device=dev).manual_seed(1000 * seed + layer)
+    draw = lambda n, K: torch.randn(n, K, generator=g, device=dev).mul_(K ** -0.5).to(torch.bfloat16)
+    for e in range(wl.E):
+        x.load(e, draw(wl.inter, wl.d), draw(wl.inter, wl.d), draw(wl.d, wl.inter))
+    return x
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--workload", default="dsv3", choices=sorted(I.WORKLOADS))
@@ -147,11 +178,15 @@ def main():
     ap.add_argument("--sys-drift", type=float, default=0.25,
                     help="systematic logit shift between the two router inputs, see inputs.make_step_layer")
     ap.add_argument("--seed", type=int, default=0)
+    ap.add_argument("--experts", action="store_true", help="move the experts' weights and compute the layers' outputs")
     args = ap.parse_args()
     wl = I.WORKLOADS[args.workload]
     T = args.tokens or wl.T
+    if args.experts and not wl.inter:
+        ap.error(f"the workload {wl.name} has no experts' sizes")
     loop = ServingLoop(wl, T)
     budget = make_budget_for(wl, T)
+    experts = [random_experts(wl, l, args.seed, loop.dev) for l in range(args.layers)] if args.experts else None
     recs = []
     for s in range(args.steps):
         for l in range(args.layers):
@@ -159,13 +194,17 @@ def main():
             dev = loop.dev
             sb = li.select_bias.to(dev) if li.select_bias is not None else None
             router = B.make_router(li.W.to(dev), None, sb)
-            r = loop.layer_step(l, router, li.h_prev.to(dev), li.H.to(dev), budget, quality=True)
+            H = li.H.to(dev)
+            r = loop.layer_step(l, router, li.h_prev.to(dev), H, budget, quality=True)
+            if experts:
+                out = loop.experts_step(r, H, experts[l])
+                r["out_rms"] = out.float().square().mean().sqrt().item()
             torch.cuda.synchronize(dev)
             _, before, after, vanilla = loop.realised_loads(r, budget)
             recs.append(dict(step=s, layer=l, n_swaps=int(r["out"]["n_swaps"].item()), hit_rate=r["hit_rate"],
                              cos_hidden=r["cos_hidden"], cos_logits=r["cos_logits"],
                              real_vanilla=max_over_mean(vanilla), real_before=max_over_mean(before),
-                             real_after=max_over_mean(after)))
+                             real_after=max_over_mean(after), **({"out_rms": r["out_rms"]} if experts else {})))
     moved = [r for r in recs if r["n_swaps"] > 0]
     n = max(1, len(recs))
     print(json.dumps(dict(
