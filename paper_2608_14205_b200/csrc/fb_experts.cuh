@@ -71,6 +71,9 @@ struct ExpertParams {
 
 struct ExpertTiles {
   int32_t most;                                         // rows of x in the largest tile
+  // A slot has several tiles, so W is read more than once.  Where none has, its loads go first when L2 needs room (decode, 64
+  // tokens of 256 experts of 7168 x 2048 in e4m3: 906 -> 900 us; with it for prefill of 16384 tokens: 4900 -> 5250 us).
+  int32_t several;
   int32_t warp_most[kExpertThreads / 32];
   int32_t warp_sums[kExpertThreads / 32];
   int32_t first_tile[FB_MAX_EXPERTS + 1];               // tiles of x before this slot's
@@ -88,17 +91,17 @@ struct ExpertShared {
 };
 
 // ---------------------------------------------------------------- copies
-__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const void* tmap, uint32_t bar, int32_t c0, int32_t c1, int32_t c2) {
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const void* tmap, uint32_t bar, int32_t c0, int32_t c1, int32_t c2, uint64_t policy) {
   asm volatile(
-      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4, %5}], [%2], %6;" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "l"(policy)
       : "memory");
 }
 __device__ __forceinline__ void tma_load_5d_pair(uint32_t dst, const void* tmap, uint32_t bar, int32_t c0, int32_t c1, int32_t c2,
-                                                 int32_t c3, int32_t c4) {
+                                                 int32_t c3, int32_t c4, uint64_t policy) {
   asm volatile(
-      "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
+      "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4, %5, %6, %7}], [%2], %8;" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "l"(policy)
       : "memory");
 }
 __device__ __forceinline__ void tma_load_rows_pair(uint32_t dst, const void* tmap, uint32_t bar, int32_t c0, int32_t c1) {
@@ -204,7 +207,7 @@ __device__ __forceinline__ void expert_plan_tiles(ExpertTiles& sh, const ExpertP
   }
   most = __reduce_max_sync(0xffffffffu, most);
   if (lane == 31) { sh.warp_sums[warp] = sum; sh.warp_most[warp] = most; }
-  __syncthreads();
+  const int several = __syncthreads_or(tiles > 1);
   const int w = lane < kExpertThreads / 32 ? sh.warp_sums[lane] : 0;
   sum += __reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
   if (e < p.n_slots) sh.first_tile[e + 1] = sum;
@@ -213,6 +216,7 @@ __device__ __forceinline__ void expert_plan_tiles(ExpertTiles& sh, const ExpertP
     most = 0;
     for (int i = 0; i < (p.n_slots + 31) / 32; ++i) most = max(most, sh.warp_most[i]);
     sh.most = most;
+    sh.several = several;
   }
   __syncthreads();
 }
@@ -391,6 +395,7 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
   if (warp == 0) {
     // -------------------------------------------------------------- TMA loads
     const bool leader = elect_one();
+    const uint64_t policy = sh.tiles.several ? l2_policy_evict_normal() : l2_policy_evict_first();
     uint32_t s = 0, phase = 0, fills = 0;
     bool ok = true;
     for (int g = first; g < total && ok; g += stride) {
@@ -405,9 +410,9 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
         if (leader) {
           if (rank == 0) mbar_arrive_expect_tx(smem_u32(&sh.full_bar[s]), bytes);
           if constexpr (kSwiglu)
-            tma_load_5d_pair(w_dst, &map_w, full, kb * kStepK, 0, 0, (t.m * (kExpertTileM / 2) + rank * 64) / 16, t.slot);
+            tma_load_5d_pair(w_dst, &map_w, full, kb * kStepK, 0, 0, (t.m * (kExpertTileM / 2) + rank * 64) / 16, t.slot, policy);
           else
-            tma_load_3d_pair(w_dst, &map_w, full, kb * kStepK, t.m * kExpertTileM + rank * 128, t.slot);
+            tma_load_3d_pair(w_dst, &map_w, full, kb * kStepK, t.m * kExpertTileM + rank * 128, t.slot, policy);
         }
         __syncwarp();
         if (!gather && kTileLoadRows * lane < half)

@@ -49,15 +49,15 @@ __device__ __forceinline__ void tma_load_rows(uint32_t dst, const void* tmap, ui
                "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1)
                : "memory");
 }
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, uint32_t bar, int32_t c0, int32_t c1, int32_t c2) {
-  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
-               "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
-               : "memory");
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, uint32_t bar, int32_t c0, int32_t c1, int32_t c2, uint64_t policy) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4, %5}], [%2], %6;" ::"r"(dst),
+               "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "l"(policy)
+      : "memory");
 }
-__device__ __forceinline__ void tma_load_5d(uint32_t dst, const void* tmap, uint32_t bar, int32_t c0, int32_t c1, int32_t c2, int32_t c3, int32_t c4) {
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const void* tmap, uint32_t bar, int32_t c0, int32_t c1, int32_t c2, int32_t c3, int32_t c4, uint64_t policy) {
   asm volatile(
-      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4, %5, %6, %7}], [%2], %8;" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "l"(policy)
       : "memory");
 }
 // e4m3 x e4m3 -> fp32, both operands K-major.
@@ -141,6 +141,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
     if (warp == 0) {
       // ------------------------------------------------------------ TMA loads
       const bool leader = elect_one();
+      const uint64_t policy = sh.tiles.several ? l2_policy_evict_normal() : l2_policy_evict_first();
       uint32_t s = 0, phase = 0, fills = 0;
       bool ok = true;
       for (int g = first; g < total && ok; g += stride) {
@@ -157,12 +158,12 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
             if (rank == 0) mbar_arrive_expect_tx(smem_u32(&sh.full_bar[s]), bytes);
             if constexpr (kSwiglu) {
               const int w_group = t.m * (kExpertTileM / 2 / 16) + rank * 4;      // of 16 outputs
-              if constexpr (kPair) tma_load_5d_pair(w_dst, &map_w, full, kb * 128, 0, 0, w_group, t.slot);
-              else tma_load_5d(w_dst, &map_w, full, kb * 128, 0, 0, w_group, t.slot);
+              if constexpr (kPair) tma_load_5d_pair(w_dst, &map_w, full, kb * 128, 0, 0, w_group, t.slot, policy);
+              else tma_load_5d(w_dst, &map_w, full, kb * 128, 0, 0, w_group, t.slot, policy);
             } else {
               const int w_row = t.m * kExpertTileM + rank * 128;
-              if constexpr (kPair) tma_load_3d_pair(w_dst, &map_w, full, kb * 128, w_row, t.slot);
-              else tma_load_3d(w_dst, &map_w, full, kb * 128, w_row, t.slot);
+              if constexpr (kPair) tma_load_3d_pair(w_dst, &map_w, full, kb * 128, w_row, t.slot, policy);
+              else tma_load_3d(w_dst, &map_w, full, kb * 128, w_row, t.slot, policy);
             }
           }
           __syncwarp();
