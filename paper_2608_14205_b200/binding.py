@@ -241,20 +241,24 @@ FB_DTYPE_BF16, FB_DTYPE_F32, FB_DTYPE_E4M3 = 0, 1, 2
 FB_ACT_NONE, FB_ACT_SWIGLU = 0, 1
 
 
+_EXPERT_DTYPES = {torch.bfloat16: (FB_DTYPE_BF16, 2), torch.float8_e4m3fn: (FB_DTYPE_E4M3, 1)}
+
+
 def make_expert_matrix(w: torch.Tensor, scale: Optional[torch.Tensor] = None, act: int = FB_ACT_NONE) -> FbExpertMatrix:
     """w: [slots, n, K] bf16 or e4m3, each slot's matrix contiguous (slots may lie further apart: parts of slot images);
     scale (e4m3): float32 [slots, row blocks, ceil(K / 128)], contiguous per slot."""
-    assert w.dim() == 3 and w.stride(2) == 1 and w.stride(1) == w.shape[2], "a slot's matrix must be contiguous"
-    assert w.dtype in (torch.bfloat16, torch.float8_e4m3fn)
-    e4m3 = w.dtype == torch.float8_e4m3fn
-    m = FbExpertMatrix(FB_DTYPE_E4M3 if e4m3 else FB_DTYPE_BF16, act, w.shape[0], w.shape[1], w.shape[2], w.data_ptr(),
-                       w.stride(0) * w.element_size(), None, 0)
+    shape, stride = w.shape, w.stride()
+    assert len(shape) == 3 and stride[2] == 1 and stride[1] == shape[2], "a slot's matrix must be contiguous"
+    kind = _EXPERT_DTYPES.get(w.dtype)
+    assert kind is not None, "bf16 or e4m3"
+    slots, n, K = shape
+    m = FbExpertMatrix(kind[0], act, slots, n, K, w.data_ptr(), stride[0] * kind[1], None, 0)
     if scale is not None:
-        rows = w.shape[1]
-        blocks = 2 * -(-(rows // 2) // 128) if act == FB_ACT_SWIGLU else -(-rows // 128)
-        assert scale.dtype == torch.float32 and scale.shape == (w.shape[0], blocks, -(-w.shape[2] // 128)), "one scale per block"
-        assert scale.stride(2) == 1 and scale.stride(1) == scale.shape[2], "a slot's scales must be contiguous"
-        m.scale, m.scale_slot = scale.data_ptr(), scale.stride(0)
+        blocks, wide = (2 * ((n // 2 + 127) // 128) if act == FB_ACT_SWIGLU else (n + 127) // 128), (K + 127) // 128
+        assert scale.dtype == torch.float32 and scale.shape == (slots, blocks, wide), "one scale per block"
+        at = scale.stride()
+        assert at[2] == 1 and at[1] == wide, "a slot's scales must be contiguous"
+        m.scale, m.scale_slot = scale.data_ptr(), at[0]
     m._keepalive = (w, scale)
     return m
 
@@ -403,17 +407,23 @@ class Context:
 
     def fb_quantize_rows(self, x, rows, n, q, scale, stream=None):
         assert x.dtype == torch.bfloat16 and scale.dtype == torch.float32
-        _check(lib().fb_quantize_rows(self._h, _ptr(x), rows, n, _ptr(q), _ptr(scale), _stream(stream)), "fb_quantize_rows")
+        st = lib().fb_quantize_rows(self._h, _ptr(x), rows, n, _ptr(q), _ptr(scale), _stream(stream))
+        if st:
+            _check(st, "fb_quantize_rows")
 
     def fb_expert_matmul(self, matrix, x, x_scale, slot_offsets, perm, rows, out, out_scale=None, stream=None):
         """x: [x_rows, K] of the matrix's type; out: [rows, n_out] bf16, or e4m3 with out_scale."""
-        assert x.dim() == 2 and x.shape[1] == matrix.K
-        _check(lib().fb_expert_matmul(self._h, ctypes.byref(matrix), _ptr(x), _ptr(x_scale), x.shape[0], _ptr(slot_offsets),
-                                      _ptr(perm), rows, _ptr(out), _ptr(out_scale), _stream(stream)), "fb_expert_matmul")
+        x_rows, K = x.shape
+        assert K == matrix.K, "rows of x: as long as the matrix's"
+        st = lib().fb_expert_matmul(self._h, ctypes.byref(matrix), _ptr(x), _ptr(x_scale), x_rows, _ptr(slot_offsets), _ptr(perm), rows,
+                                    _ptr(out), _ptr(out_scale), _stream(stream))
+        if st:
+            _check(st, "fb_expert_matmul")
 
     def fb_combine(self, rows, w, inv_perm, T, n, addend, out, stream=None):
-        _check(lib().fb_combine(self._h, _ptr(rows), _ptr(w), _ptr(inv_perm), T, n, _ptr(addend), _ptr(out), _stream(stream)),
-               "fb_combine")
+        st = lib().fb_combine(self._h, _ptr(rows), _ptr(w), _ptr(inv_perm), T, n, _ptr(addend), _ptr(out), _stream(stream))
+        if st:
+            _check(st, "fb_combine")
 
     def fb_device_status(self, stream=None) -> int:
         word = ctypes.c_int32(0)

@@ -116,11 +116,12 @@ struct fb_ctx {
 namespace {
 
 struct DeviceGuard {
-  int prev = -1;
+  int prev = -1;                  // the device to go back to (-1: it was the current one already)
   bool ok = true;
   explicit DeviceGuard(int dev) {
-    if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-    if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
+    if (cudaGetDevice(&prev) != cudaSuccess) { prev = -1; ok = false; return; }
+    if (prev == dev) prev = -1;
+    else if (cudaSetDevice(dev) != cudaSuccess) ok = false;
   }
   ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
 };
@@ -1219,8 +1220,8 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   const cuuint32_t width = static_cast<cuuint32_t>(step);
   // one slot has no stride: any value that the map takes
   const cuuint64_t slot_bytes = m->n_slots > 1 ? m->slot_bytes : (row_bytes * static_cast<uint64_t>(m->n) + 15) / 16 * 16;
-  bool ok;
-  {
+  bool ok = true;
+  if (perm == nullptr) {
     const cuuint64_t size[2] = {K, static_cast<cuuint64_t>(x_rows)}, stride[1] = {row_bytes};
     const cuuint32_t box[2] = {width, fb::kTileLoadRows};
     ok = encode(&map_x, 2, x, size, stride, box);
@@ -1255,7 +1256,7 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = pair ? 2 : 1;
-  const cudaError_t err = launch_refused(ctx) ? cudaErrorUnknown : cudaLaunchKernelEx(&cfg, kernel.fn, map_x, map_w, p);
+  const cudaError_t err = launch_refused(ctx) ? cudaErrorUnknown : cudaLaunchKernelEx(&cfg, kernel.fn, perm == nullptr ? map_x : map_w, map_w, p);
   return err == cudaSuccess ? FB_OK : FB_ERR_CUDA;
 }
 

@@ -369,7 +369,7 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
       mbar_init(smem_u32(&sh.acc_empty[a]), 2 * kExpertEpilogueWarps);
     }
     fence_mbar_init();
-    prefetch_tensormap(&map_x);
+    if (!gather) prefetch_tensormap(&map_x);           // (a gather has none)
     prefetch_tensormap(&map_w);
   }
   if (warp == 1) {

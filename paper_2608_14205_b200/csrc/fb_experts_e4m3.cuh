@@ -115,7 +115,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
     }
     for (int q = 0; q < 4; ++q) mbar_init(smem_u32(&sh.top_bar[q]), 2);
     fence_mbar_init();
-    prefetch_tensormap(&map_x);
+    if (!gather) prefetch_tensormap(&map_x);
     prefetch_tensormap(&map_w);
   }
   if (warp == 1) {
