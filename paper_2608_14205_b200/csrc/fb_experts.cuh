@@ -122,6 +122,11 @@ __device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.
 __device__ __forceinline__ void mbar_arrive_pair(uint32_t bar, uint32_t rank) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(map_to_cta(bar, rank)) : "memory");
 }
+// The same when pred != 0; a predicated copy, not a branch.
+__device__ __forceinline__ void cp_async_16_if(uint32_t pred, uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %3, 0;\n@p cp.async.cg.shared.global [%0], [%1], 16, %2;\n}\n" ::"r"(dst), "l"(src), "r"(bytes), "r"(pred)
+               : "memory");
+}
 // Arrives at the barrier once the thread's copies so far are complete.
 __device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
@@ -288,37 +293,46 @@ __device__ __forceinline__ void gather_rows(const ExpertParams& p, int total, in
   const int row0 = (static_cast<int>(threadIdx.x >> 5) - kExpertFirstGatherWarp) * 4 + (lane >> 3);
   const uint32_t row_bytes = static_cast<uint32_t>(p.row_bytes);
   const uint32_t to = x_tiles + static_cast<uint32_t>(row0 * 128 + ((unit ^ (row0 & 7)) << 4));        // (16 i rows on: same swizzle)
+  // 16 bytes of the last k-block that lie behind the row's end are zeros
+  const bool tail = static_cast<uint32_t>(p.num_kb - 1) * 128u + 16u * unit < row_bytes;
   uint32_t s = 0, phase = 0;
   bool ok = true;
-  int32_t rows[kGatherRows], next_rows[kGatherRows];
+  int32_t rows[kGatherRows];
 #pragma unroll
-  for (int i = 0; i < kGatherRows; ++i) next_rows[i] = kNoRow;
-  if (first < total) rows_of(first, row0, next_rows);
+  for (int i = 0; i < kGatherRows; ++i) rows[i] = kNoRow;
+  if (first < total) rows_of(first, row0, rows);
   for (int g = first; g < total && ok; g += stride) {
+    const uint8_t* src[kGatherRows];
+    uint32_t some = 0, zero = 0;                         // rows i to copy, to clear
 #pragma unroll
-    for (int i = 0; i < kGatherRows; ++i) rows[i] = next_rows[i];
-    bool any_zero = false;
-#pragma unroll
-    for (int i = 0; i < kGatherRows; ++i) any_zero = any_zero || rows[i] == kZeroRow;
+    for (int i = 0; i < kGatherRows; ++i) {
+      src[i] = static_cast<const uint8_t*>(p.x) + static_cast<uint64_t>(static_cast<uint32_t>(max(rows[i], 0))) * row_bytes + 16u * unit;
+      some |= (rows[i] >= 0 ? 1u : 0u) << i;
+      zero |= (rows[i] == kZeroRow ? 1u : 0u) << i;
+    }
+    const bool whole = __all_sync(0xffffffffu, some == (1u << kGatherRows) - 1);
     for (int kb = 0; kb < p.num_kb; ++kb) {
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&empty_bar[s]), phase ^ 1u, abort_flag));
       if (!ok) break;
-      const uint32_t at = static_cast<uint32_t>(kb) * 128u + 16u * unit;
-      const bool inside = at < row_bytes;
-      const uint8_t* src = static_cast<const uint8_t*>(p.x) + (inside ? at : 0u);
+      const bool inside = kb + 1 < p.num_kb || tail;
+      const uint32_t bytes = inside ? 16u : 0u, at = inside ? static_cast<uint32_t>(kb) * 128u : 0u, dst = to + s * stage_bytes;
+      if (whole) {
 #pragma unroll
-      for (int i = 0; i < kGatherRows; ++i)
-        if (rows[i] >= 0)
-          cp_async_16(to + s * stage_bytes + 2048u * i, src + static_cast<uint64_t>(static_cast<uint32_t>(rows[i])) * row_bytes, inside ? 16u : 0u);
-      if (kb < static_cast<int>(stages) && any_zero) {   // zeros stay for the tile's later uses of the stage
+        for (int i = 0; i < kGatherRows; ++i) cp_async_16(dst + 2048u * i, src[i] + at, bytes);
+      } else {
 #pragma unroll
         for (int i = 0; i < kGatherRows; ++i)
-          if (rows[i] == kZeroRow) st_shared_v4(to + s * stage_bytes + 2048u * i, 0u, 0u, 0u, 0u);
+          cp_async_16_if(some & (1u << i), dst + 2048u * i, src[i] + at, bytes);
+        if (kb < static_cast<int>(stages) && zero != 0) {      // zeros stay for the tile's later uses of the stage
+#pragma unroll
+          for (int i = 0; i < kGatherRows; ++i)
+            if ((zero >> i) & 1u) st_shared_v4(dst + 2048u * i, 0u, 0u, 0u, 0u);
+        }
+        __syncwarp();
       }
-      __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&x_bar[s]));   // (the zeros; the copies report for themselves)
       cp_async_arrive(smem_u32(&x_bar[s]));
-      if (kb == 0 && g + stride < total) rows_of(g + stride, row0, next_rows);      // these numbers arrive meanwhile
+      if (kb == 0 && g + stride < total) rows_of(g + stride, row0, rows);      // these numbers arrive meanwhile
       if (++s == stages) { s = 0; phase ^= 1u; }
     }
   }
