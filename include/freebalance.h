@@ -16,6 +16,8 @@
  *   4. fb_route_dispatch    normal router pass g_l(H_l) (Eq. 3), authoritative top-k
  *                           and routing weights, and the token -> expert dispatch
  *                           index under the committed placement pi'
+ *      fb_quantize_rows, fb_expert_matmul, fb_combine
+ *                           the experts behind that index: their products and the weighted sum
  *
  * Expert-parallel ranks are logical: a placement maps expert e to a physical slot
  * p = expert_to_slot[e] in [0, E); slot p belongs to rank p / (E / R).  Everything
@@ -29,7 +31,7 @@
  *     fb_layer_step_host and fb_device_status, which block until the stream drains,
  *     fb_apply_swaps_staged (waits for the plan) and fb_calibrate_exchange (times itself).
  *   - The method's device calls (fb_predict_load, fb_plan_swaps, fb_predict_and_plan,
- *     fb_route_dispatch, fb_layer_step, the dispatch-index helpers) allocate nothing,
+ *     fb_route_dispatch, fb_layer_step, the dispatch-index helpers, the experts' calls) allocate nothing,
  *     query nothing and keep no per-launch state on the host that a kernel depends on,
  *     so after one ordinary call with the same arguments (which builds the tensor maps
  *     and loads the kernels) they may be captured into a CUDA graph and the graph
@@ -68,7 +70,8 @@ typedef enum {
   FB_ERR_CUDA = 3,                         /* a CUDA runtime / driver call failed             */
   FB_ERR_BAD_PLACEMENT = 4,                /* device: expert_to_slot is not a bijection       */
   FB_ERR_TIMEOUT = 5,                      /* device: a bounded wait inside a kernel expired  */
-  FB_ERR_RANGE = 6,                        /* device: sum of counts exceeds FB_MAX_COUNT_SUM  */
+  FB_ERR_RANGE = 6,                        /* device: sum of counts exceeds FB_MAX_COUNT_SUM, or */
+                                           /* an offset or index that a call reads is out of range */
   FB_ERR_INTERNAL = 7                      /* device, builds with -DFB_DEBUG only: an index the */
                                            /* kernels were about to write was out of range      */
 } fb_status;
@@ -420,10 +423,12 @@ fb_status fb_apply_swaps_staged(fb_ctx* ctx, void* slot_weights, uint64_t expert
  *   out[t] = sum over j of topk_w[t][j] * y[inv_perm[t k + j]]   fb_combine
  * Weights are bf16, or e4m3 with a scale for each block of 128 x 128; the rows that meet e4m3 weights are e4m3 with a
  * scale for each 128 columns (fb_quantize_rows; the SwiGLU product can hand out such rows itself).  Forward only: router
- * and experts are frozen here.  A row's
- * result does not depend on the rows beside it, and equal calls give equal bits.
+ * and experts are frozen here.  A row's result does not depend on the rows beside it, nor on its position, and equal
+ * calls give equal bits.
  * All three run on ctx's device, allocate nothing, use no scratch of the context (calls may overlap on any streams) and
- * may be captured.  Sums, norms and scales are formed in 32 bits. */
+ * may be captured (tensor maps travel with the launch).  Sums, maxima and scales are formed in 32 bits.  Errors:
+ * FB_ERR_INVALID_ARG, FB_ERR_UNSUPPORTED_SHAPE (a limit below, or sizes whose launch would pass 2^31 blocks),
+ * FB_ERR_CUDA; device status as named at each call. */
 
 typedef enum {
   FB_ACT_NONE = 0,
@@ -461,14 +466,14 @@ fb_status fb_quantize_rows(fb_ctx* ctx, const void* x, int64_t rows, int32_t n, 
  *   x_scale       dev f32 [x_rows][ceil(K / 128)] (e4m3), else NULL
  *   slot_offsets  dev u32 [n_slots + 1] as written by fb_route_dispatch; a rank that holds the slots from s0 on passes
  *                 slot_offsets + s0 and its own matrices.  NULL: one slot (n_slots 1) that has all rows
- *   perm          dev i32, indexed by p, or NULL
+ *   perm          dev i32 [x_rows k], indexed by p, or NULL
  *   rows          rows that out holds; slot_offsets[n_slots] - slot_offsets[0] may be less, and rows of out behind it
  *                 are left as they are.  Slots may be empty.
- *   out           dev bf16 [rows][n_out], n_out = n (n / 2 with FB_ACT_SWIGLU), rounded once from 32 bits; with out_scale
- *                 (e4m3 and FB_ACT_SWIGLU only) e4m3 [rows][n_out], quantised as by fb_quantize_rows from the 32-bit values
+ *   out           dev bf16 [rows][n_out], n_out = n (n / 2 with FB_ACT_SWIGLU), rounded once from 32 bits (silu(g) is
+ *                 taken as 0 for g below -87); with out_scale (e4m3 and FB_ACT_SWIGLU only) e4m3 [rows][n_out], quantised as by fb_quantize_rows from the 32-bit values
  *   out_scale     dev f32 [rows][ceil(n_out / 128)] or NULL
- * out overlaps no input.  One launch.  Device status FB_ERR_RANGE: offsets that do not rise or pass `rows` (that
- * slot's rows are left out), an entry of perm outside x (row 0 is read instead). */
+ * out overlaps no input.  One launch.  Device status FB_ERR_RANGE: offsets that do not rise, pass `rows` or
+ * (with perm) x_rows k (that slot's rows are left out), an entry of perm outside x (row 0 is read instead). */
 fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* matrix, const void* x, const float* x_scale, int32_t x_rows,
                            const uint32_t* slot_offsets, const int32_t* perm, int32_t rows, void* out, float* out_scale,
                            fb_stream stream);

@@ -161,6 +161,7 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
   const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
   return lo | hi << 16;
 }
+// (__fdividef gives 0 for a divisor above 2^126: silu(g) is 0 for g below -87)
 __device__ __forceinline__ float swiglu(float g, float u) { return __fdividef(g, 1.0f + __expf(-g)) * u; }
 
 // ---------------------------------------------------------------- tiles
@@ -191,7 +192,8 @@ __device__ __forceinline__ void expert_plan_tiles(ExpertTiles& sh, const ExpertP
     int first = 0, count = p.rows;
     if (p.slot_offsets != nullptr) {
       const uint32_t lo = p.slot_offsets[e], hi = p.slot_offsets[e + 1];
-      if (base <= lo && lo <= hi && hi - base <= static_cast<uint32_t>(p.rows)) {
+      const uint64_t positions = p.perm != nullptr ? static_cast<uint64_t>(p.x_rows) * static_cast<uint32_t>(p.k) : UINT32_MAX;
+      if (base <= lo && lo <= hi && hi - base <= static_cast<uint32_t>(p.rows) && hi <= positions) {
         first = static_cast<int>(lo - base);
         count = static_cast<int>(hi - lo);
       } else {
@@ -608,7 +610,7 @@ constexpr int kCombineThreads = 128;
 template <int kK>
 __global__ void __launch_bounds__(kCombineThreads)
 fb_combine_kernel(const __nv_bfloat16* __restrict__ rows, const float* __restrict__ w, const int32_t* __restrict__ inv_perm, int T, int n,
-                  int pieces, const __nv_bfloat16* __restrict__ addend, __nv_bfloat16* __restrict__ out, int32_t* status) {
+                  int pieces, const __nv_bfloat16* addend, __nv_bfloat16* out, int32_t* status) {      // (addend may be out)
   pdl_wait();
   pdl_launch_dependents();
   const int t = static_cast<int>(blockIdx.x) / pieces, piece = static_cast<int>(blockIdx.x) - t * pieces;

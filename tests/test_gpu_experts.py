@@ -295,6 +295,10 @@ def test_bad_offsets_and_rows_are_reported_and_nothing_else_is_written(e4m3):
     run()
     assert ctx.fb_device_status() == B.FB_ERR_RANGE
     assert torch.equal(out[:20], want[:20]) and (out[20:] == 7.0).all()
+    c.offsets.copy_(good + 1000)                             # positions that perm cannot have
+    out.fill_(7.0)
+    run()
+    assert ctx.fb_device_status() == B.FB_ERR_RANGE and (out == 7.0).all()
     c.offsets.copy_(good)
     c.perm[25], c.perm[26] = -5, 10 ** 9                     # outside x: row 0 instead
     run()
