@@ -415,6 +415,7 @@ class Context:
         """x: [x_rows, K] of the matrix's type; out: [rows, n_out] bf16, or e4m3 with out_scale."""
         x_rows, K = x.shape
         assert K == matrix.K, "rows of x: as long as the matrix's"
+        assert out is None or out.element_size() == (2 if out_scale is None else 1), "bf16 results, e4m3 ones with out_scale"
         st = lib().fb_expert_matmul(self._h, ctypes.byref(matrix), _ptr(x), _ptr(x_scale), x_rows, _ptr(slot_offsets), _ptr(perm), rows,
                                     _ptr(out), _ptr(out_scale), _stream(stream))
         if st:

@@ -1206,8 +1206,9 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   // 5046 us; 1024 rows 1385 and 1363; 2048 rows 670 and 648; 8192 rows of one 8192 x 8192 matrix 565 and 530.
   const bool pair = !e4m3 || rows / m->n_slots >= 1024;
   // a slot of c rows has at most ceil(c / tile) tiles of rows
-  const int64_t tiles = (rows / (pair ? 256 : 128) + (m->n_slots < rows ? m->n_slots : rows)) * static_cast<int64_t>(p.m_blocks);
-  if (tiles >= (int64_t{1} << 31)) return FB_ERR_UNSUPPORTED_SHAPE;
+  p.max_tiles = rows / (pair ? 256 : 128) + (m->n_slots < rows ? m->n_slots : rows);
+  const int64_t tiles = p.max_tiles * static_cast<int64_t>(p.m_blocks);
+  if (tiles > (int64_t{1} << 30)) return FB_ERR_UNSUPPORTED_SHAPE;
   CUtensorMap map_x, map_w;
   const CUtensorMapDataType type = e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   auto encode = [&](CUtensorMap* map, int dims, const void* ptr, const cuuint64_t* size, const cuuint64_t* stride, const cuuint32_t* box) {

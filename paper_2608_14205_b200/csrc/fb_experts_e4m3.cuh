@@ -87,6 +87,10 @@ __device__ __forceinline__ void fma_two(float& d0, float& d1, uint32_t a0, uint3
       : "+f"(d0), "+f"(d1)
       : "r"(a0), "r"(a1), "f"(s));
 }
+// What a k-block takes (cycles; 8192 x 8192 x 8192): its MMAs 516, with the hand-overs of the accumulators 588, with the loads
+// 660, with the read-out of TMEM 666, with the multiply-adds 805 - the chain wait, read, add, release of the eight warps, whose pipe
+// is 32 % busy.  Up projection with SwiGLU and quantised results, 256 experts of 7168 x 2048: 16384 tokens 4.3 ms (1796 TFLOP/s)
+// in short runs, 4.8 - 5.0 ms at 1000 W; 64 tokens 900 us, 6.6 TB/s (a copy: 6.53), and 935 - 970 us at 1000 W.
 template <bool kPair, bool kSwiglu, bool kQuantize>
 __global__ void __launch_bounds__(kExpertThreads, 1)
 fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
@@ -131,8 +135,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
   const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem_base, 0);      // (warp-uniform for the compiler as well)
   uint32_t base;
   int slot = 0;                                          // of the warp's last tile
-  expert_plan_tiles<L::kRows>(sh.tiles, p, base);
-  const int total = sh.tiles.first_tile[p.n_slots] * p.m_blocks;
+  const int total = expert_plan_tiles<L::kRows>(sh.tiles, p, base);
   const int stride = static_cast<int>(gridDim.x) / kGroup, first = static_cast<int>(blockIdx.x) / kGroup;
 
   // Registers: 256 threads with 208 and 256 with 48 are the 512 x 128 of the launch.

@@ -295,6 +295,13 @@ def test_bad_offsets_and_rows_are_reported_and_nothing_else_is_written(e4m3):
     run()
     assert ctx.fb_device_status() == B.FB_ERR_RANGE
     assert torch.equal(out[:20], want[:20]) and (out[20:] == 7.0).all()
+    many = Case([20] * 40, 64, 64, e4m3, False, False, seed=6, whole=True, k=1)       # every other slot claims all rows
+    many.offsets[:40:2], many.offsets[1::2] = 0, 800
+    big = torch.full((800, 64), 7.0, dtype=torch.bfloat16, device=DEV)
+    ctx.fb_expert_matmul(many.matrix(), many.x, many.xs, many.offsets, None, 800, big)
+    torch.cuda.synchronize()
+    assert ctx.fb_device_status() == B.FB_ERR_RANGE
+    assert (big == 7.0).all()
     c.offsets.copy_(good + 1000)                             # positions that perm cannot have
     out.fill_(7.0)
     run()
@@ -456,7 +463,7 @@ def test_refusals():
     matmul(A, f8(2, 32, 64), None, x=f8(8, 64), xs=f32(8, 1), out=bf(8, 32))               # e4m3 without scales
     matmul(A, f8(2, 32, 64), f32(2, 1, 1), x=f8(8, 64), out=bf(8, 32))
     matmul(A, **{**good, "x": bf(8, 64)}, xs=f32(8, 1))                                    # bf16 with scales
-    matmul(A, **good, out_scale=f32(8, 1))                                                 # bf16 results are not quantised
+    matmul(A, **{**good, "out": f8(8, 32)}, out_scale=f32(8, 1))                            # bf16 operands give bf16 results
     matmul(A, f8(2, 32, 64), f32(2, 1, 1), x=f8(8, 64), xs=f32(8, 1), out=f8(8, 32), out_scale=f32(8, 1))   # nor without SwiGLU
     matmul(A, **good, offsets=None)                                                        # two slots without offsets
     matmul(A, **{**good, "x": bf(7, 64)})                                                  # fewer rows of x than of out

@@ -159,6 +159,45 @@ def test_a_rank_of_the_placement_by_itself():
     loop.close()
 
 
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_captured_chain_follows_new_tokens(e4m3):
+    # route, quantise, up, down, combine in one graph; replayed on other hidden states, whose routing differs
+    wl = small("qwen3", e4m3, 512, 128)
+    T, k = 700, wl.k
+    layers = [I.make_layer(wl, l, 0, T=T) for l in range(2)]
+    ctx = B.Context(T, wl.d, wl.E, k, wl.R, wl.gate, wl.n_group, wl.topk_group, wl.renorm, wl.route_scale)
+    x = S.random_experts(wl, 0, 9, DEV)
+    buf = X.ExpertBuffers(x, T, k)
+    router = B.make_router(layers[0].W.to(DEV), None, None)
+    pi = layers[0].expert_to_slot.to(DEV)
+    H = layers[0].H.to(DEV)
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32, device=DEV)
+    ids, w, offsets, ranks, perm, inv, load = i32(T * k), torch.zeros(T * k, device=DEV), i32(wl.E + 1), i32(wl.R + 1), i32(T * k), i32(T * k), i32(wl.R)
+
+    def chain():
+        ctx.fb_route_dispatch(router, H, T, pi, ids, w, offsets, ranks, perm, inv, load)
+        return X.run_experts(ctx, x, buf, H, T, k, w, offsets, perm, inv)
+
+    chain()
+    torch.cuda.synchronize()
+    first_ids = ids.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = chain()
+    H.copy_(layers[1].H.to(DEV))
+    out.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    got, got_ids = out.clone(), ids.clone()
+    assert not torch.equal(got_ids, first_ids)
+    out.zero_()
+    chain()
+    torch.cuda.synchronize()
+    assert torch.equal(got_ids, ids) and torch.equal(got, out) and got.abs().sum() > 0
+    assert ctx.fb_device_status() == 0
+    ctx.close()
+
+
 @pytest.mark.parametrize("name", ["qwen3", "dsv3"])
 def test_serving_loop_with_experts_from_the_command_line(name, monkeypatch, capsys):
     import json
