@@ -517,17 +517,22 @@ struct ExpertKernel {
   ExpertKernelFn fn;
   size_t smem;
 };
-template <bool kPair>
+template <bool kPair, bool kSplit>
 ExpertKernel e4m3_kernel(bool swiglu, bool quantize) {
   constexpr size_t kSmem = fb::ExpertE4m3Layout<kPair>::kDynamic;
-  if (!swiglu) return {fb::fb_expert_matmul_e4m3_kernel<kPair, false, false>, kSmem};
-  if (!quantize) return {fb::fb_expert_matmul_e4m3_kernel<kPair, true, false>, kSmem};
-  return {fb::fb_expert_matmul_e4m3_kernel<kPair, true, true>, kSmem};
+  if (!swiglu) return {fb::fb_expert_matmul_e4m3_kernel<kPair, false, false, kSplit>, kSmem};
+  if (!quantize) return {fb::fb_expert_matmul_e4m3_kernel<kPair, true, false, kSplit>, kSmem};
+  return {fb::fb_expert_matmul_e4m3_kernel<kPair, true, true, kSplit>, kSmem};
 }
-ExpertKernel expert_kernel(bool e4m3, bool pair, bool swiglu, bool quantize) {
-  if (e4m3) return pair ? e4m3_kernel<true>(swiglu, quantize) : e4m3_kernel<false>(swiglu, quantize);
-  if (swiglu) return {fb::fb_expert_matmul_kernel<true>, fb::ExpertLayout<true>::kDynamic};
-  return {fb::fb_expert_matmul_kernel<false>, fb::ExpertLayout<false>::kDynamic};
+template <bool kSplit>
+ExpertKernel bf16_kernel(bool swiglu) {
+  if (swiglu) return {fb::fb_expert_matmul_kernel<true, kSplit>, fb::ExpertLayout<true>::kDynamic};
+  return {fb::fb_expert_matmul_kernel<false, kSplit>, fb::ExpertLayout<false>::kDynamic};
+}
+ExpertKernel expert_kernel(bool e4m3, bool pair, bool split, bool swiglu, bool quantize) {
+  if (!e4m3) return split ? bf16_kernel<true>(swiglu) : bf16_kernel<false>(swiglu);
+  if (pair) return e4m3_kernel<true, false>(swiglu, quantize);
+  return split ? e4m3_kernel<false, true>(swiglu, quantize) : e4m3_kernel<false, false>(swiglu, quantize);
 }
 
 // A fixed one-swap plan over two slots for fb_calibrate_exchange: [placement: 2][swap: 4][n: 1].
@@ -663,8 +668,11 @@ static fb_status set_up_device(fb_ctx* ctx, int device, const DeviceLimits& dev)
   const int plan_general = raise(reinterpret_cast<const void*>(fb::fb_plan_kernel<true>));
   const int plan_uniform = raise(reinterpret_cast<const void*>(fb::fb_plan_kernel<false>));
   ctx->own_sm.smem = plan_general < plan_uniform ? plan_general : plan_uniform;
-  for (int i = 0; i < 8; ++i)                             // bf16; e4m3 single, pair: without SwiGLU, with it, quantised
-    raise(reinterpret_cast<const void*>((i < 2 ? expert_kernel(false, true, i == 1, false) : expert_kernel(true, i >= 5, (i - 2) % 3 != 0, (i - 2) % 3 == 2)).fn));
+  for (int split = 0; split < 2; ++split) {
+    for (int i = 0; i < 2; ++i) raise(reinterpret_cast<const void*>(expert_kernel(false, true, split != 0, i != 0, false).fn));
+    for (int i = 0; i < 6; ++i)                           // single blocks, pairs: without SwiGLU, with it, quantised
+      raise(reinterpret_cast<const void*>(expert_kernel(true, i >= 3, split != 0, i % 3 != 0, i % 3 == 2).fn));
+  }
   int least = 0;
   ok = ok && cudaDeviceGetStreamPriorityRange(&least, &ctx->own_sm.priority) == cudaSuccess;
   if (!ok) { cudaGetLastError(); return FB_ERR_CUDA; }
@@ -1240,11 +1248,19 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   if (!ok) return FB_ERR_CUDA;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return FB_ERR_CUDA;
-  const ExpertKernel kernel = expert_kernel(e4m3, pair, swiglu, out_scale != nullptr);
-  const int64_t at_once = pair ? ctx->max_clusters[1] : ctx->n_sm, workers = tiles < at_once ? tiles : at_once;      // blocks, or pairs of them
+  // Few tiles: clusters of up to 8 blocks share them (see KRange), as many pieces as leave each four k-blocks.
+  const int blocks_per_piece = pair ? 2 : 1;
+  p.pieces = 1;
+  if (!e4m3 || !pair)
+    for (int pieces = 8 / blocks_per_piece; pieces > 1 && p.pieces == 1; pieces /= 2)
+      if (tiles <= ctx->max_clusters[pieces * blocks_per_piece / 2] && p.num_kb >= 4 * pieces) p.pieces = pieces;
+  const bool split = p.pieces > 1;
+  const ExpertKernel kernel = expert_kernel(e4m3, pair, split, swiglu, out_scale != nullptr);
+  const int64_t at_once = split ? tiles : pair ? ctx->max_clusters[1] : ctx->n_sm, workers = tiles < at_once ? tiles : at_once;
+  const unsigned cluster = static_cast<unsigned>(blocks_per_piece * p.pieces);
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3(static_cast<unsigned>(pair ? 2 * workers : workers), 1, 1);
+  cfg.gridDim = dim3(static_cast<unsigned>(workers) * cluster, 1, 1);
   cfg.blockDim = dim3(fb::kExpertThreads, 1, 1);
   cfg.dynamicSmemBytes = kernel.smem;
   cfg.stream = static_cast<cudaStream_t>(stream_);
@@ -1252,11 +1268,11 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.x = cluster;
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = pair ? 2 : 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   const cudaError_t err = launch_refused(ctx) ? cudaErrorUnknown : cudaLaunchKernelEx(&cfg, kernel.fn, perm == nullptr ? map_x : map_w, map_w, p);
   return err == cudaSuccess ? FB_OK : FB_ERR_CUDA;
 }

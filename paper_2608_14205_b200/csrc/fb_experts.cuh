@@ -68,7 +68,29 @@ struct ExpertParams {
   int32_t m_blocks;                // tiles of W per slot
   int32_t scale_k;                 // ceil(K / 128)
   int32_t max_tiles;               // tiles of x that rising offsets can give
+  int32_t pieces;                  // split launches: blocks (pairs) of a cluster that share a tile's K
 };
+
+// Split launches.  A call with fewer tiles than the GPU has blocks (or pairs) for is latency: one tile's k-blocks one after the
+// other.  There a cluster shares the tile, each block (pair) a range of K; the partial sums go through the rings, which
+// are done with by then, and are added up in the order of the pieces by the block that stores the result.
+struct KRange {
+  int begin, end;                  // k-blocks
+};
+__device__ __forceinline__ KRange k_range(const ExpertParams& p, int piece) {
+  return {static_cast<int>(static_cast<long long>(p.num_kb) * piece / p.pieces), static_cast<int>(static_cast<long long>(p.num_kb) * (piece + 1) / p.pieces)};
+}
+// All threads of a cluster, warp by warp, wherever they are.
+__device__ __forceinline__ void cluster_meet() {
+  __syncwarp();
+  cluster_arrive();
+  cluster_wait();
+}
+__device__ __forceinline__ float4 ld_cluster_v4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
 
 struct ExpertTiles {
   int32_t most;                                         // rows of x in the largest tile
@@ -294,7 +316,7 @@ struct ExpertLayout {
 // thread's rows row0 + 16 i of the block's 128 (kNoRow: nothing is written, kZeroRow: zeros are), whose 16 bytes each go to
 // the stage's tile of 128-byte rows in the 128-byte swizzle.  x_bar[s] counts the threads whose copies are complete and the warps.
 template <typename Rows>
-__device__ __forceinline__ void gather_rows(const ExpertParams& p, int total, int first, int stride, uint32_t x_tiles, uint32_t stages,
+__device__ __forceinline__ void gather_rows(const ExpertParams& p, KRange k, int total, int first, int stride, uint32_t x_tiles, uint32_t stages,
                                             uint32_t stage_bytes, uint64_t* empty_bar,
                                             uint64_t* x_bar, volatile int* abort_flag, Rows rows_of) {
   const int lane = threadIdx.x & 31, unit = lane & 7;
@@ -319,7 +341,7 @@ __device__ __forceinline__ void gather_rows(const ExpertParams& p, int total, in
       zero |= (rows[i] == kZeroRow ? 1u : 0u) << i;
     }
     const bool whole = __all_sync(0xffffffffu, some == (1u << kGatherRows) - 1);
-    for (int kb = 0; kb < p.num_kb; ++kb) {
+    for (int kb = k.begin; kb < k.end; ++kb) {
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&empty_bar[s]), phase ^ 1u, abort_flag));
       if (!ok) break;
       const bool inside = kb + 1 < p.num_kb || tail;
@@ -331,7 +353,7 @@ __device__ __forceinline__ void gather_rows(const ExpertParams& p, int total, in
 #pragma unroll
         for (int i = 0; i < kGatherRows; ++i)
           cp_async_16_if(some & (1u << i), dst + 2048u * i, src[i] + at, bytes);
-        if (kb < static_cast<int>(stages) && zero != 0) {      // zeros stay for the tile's later uses of the stage
+        if (kb - k.begin < static_cast<int>(stages) && zero != 0) {      // zeros stay for the tile's later uses of the stage
 #pragma unroll
           for (int i = 0; i < kGatherRows; ++i)
             if ((zero >> i) & 1u) st_shared_v4(dst + 2048u * i, 0u, 0u, 0u, 0u);
@@ -340,7 +362,7 @@ __device__ __forceinline__ void gather_rows(const ExpertParams& p, int total, in
       }
       if (lane == 0) mbar_arrive(smem_u32(&x_bar[s]));   // (the zeros; the copies report for themselves)
       cp_async_arrive(smem_u32(&x_bar[s]));
-      if (kb == 0 && g + stride < total) rows_of(g + stride, row0, rows);      // these numbers arrive meanwhile
+      if (kb == k.begin && g + stride < total) rows_of(g + stride, row0, rows);      // these numbers arrive meanwhile
       if (++s == stages) { s = 0; phase ^= 1u; }
     }
   }
@@ -349,12 +371,12 @@ __device__ __forceinline__ void gather_rows(const ExpertParams& p, int total, in
 
 // One warp's part: gathered rows that have arrived are made visible to the tensor core and reported.
 template <typename Arrive>
-__device__ __forceinline__ void pass_on_rows(const ExpertParams& p, int total, int first, int stride, uint32_t stages, uint64_t* x_bar,
+__device__ __forceinline__ void pass_on_rows(KRange k, int total, int first, int stride, uint32_t stages, uint64_t* x_bar,
                                              volatile int* abort_flag, Arrive arrive) {
   uint32_t s = 0, phase = 0;
   bool ok = true;
   for (int g = first; g < total && ok; g += stride)
-    for (int kb = 0; kb < p.num_kb; ++kb) {
+    for (int kb = k.begin; kb < k.end; ++kb) {
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&x_bar[s]), phase, abort_flag));
       if (!ok) break;
       fence_proxy_async();
@@ -369,7 +391,7 @@ __device__ __forceinline__ void pass_on_rows(const ExpertParams& p, int total, i
 // 860 - 900.  Ragged ones lose what small tiles cost (8192 tokens, slots of 150 - 2000 rows: 353 and 425 us, 1168 and 970).  Few rows
 // are bound by the stream of W: 40 tokens, down projection, 56.5 us, 6.2 TB/s of 6.5 measured; one token, 50 MB, 13.4 us, of
 // which 8.6 are the stream (96 SMs have tiles), the rest launch, offsets, row numbers and the way out one after the other.
-template <bool kSwiglu>
+template <bool kSwiglu, bool kSplit>
 __global__ void __launch_bounds__(kExpertThreads, 1)
 fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                         const __grid_constant__ ExpertParams p) {
@@ -379,7 +401,8 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
   __shared__ ExpertShared sh;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
   const int lane = threadIdx.x & 31;
-  const int rank = static_cast<int>(cluster_ctarank());
+  const uint32_t cluster_rank = cluster_ctarank(), leader_rank = cluster_rank & ~1u;
+  const int rank = static_cast<int>(cluster_rank & 1u), piece = kSplit ? static_cast<int>(cluster_rank >> 1) : 0;
   const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
   volatile int* abort_flag = &sh.abort_flag;
   const bool gather = p.perm != nullptr;
@@ -413,7 +436,9 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
   uint32_t base;
   int slot = 0;                                          // of the warp's last tile
   const int total = expert_plan_tiles<kExpertTileN>(sh.tiles, p, base);
-  const int stride = static_cast<int>(gridDim.x) / 2, first = static_cast<int>(blockIdx.x) / 2;
+  const int sharers = kSplit ? 2 * p.pieces : 2;         // blocks per tile
+  const int stride = static_cast<int>(gridDim.x) / sharers, first = static_cast<int>(blockIdx.x) / sharers;
+  const KRange kr = kSplit ? k_range(p, piece) : KRange{0, p.num_kb};
   // Few rows per tile leave room for more stages: what is under way is W, and a launch of few tiles has few blocks to ask for it.
   const uint32_t stage_bytes = kExpertWBytes + 64u * static_cast<uint32_t>(max(sh.tiles.most, kExpertStepN));
   const uint32_t stages = min(kExpertRingBytes / stage_bytes, static_cast<uint32_t>(kExpertStages));
@@ -428,11 +453,11 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
       const ExpertTile t = expert_tile<kExpertTileN>(sh.tiles, p, g, slot);
       const int half = t.n / 2, x_row = t.row + rank * half + kTileLoadRows * lane;
       const uint32_t bytes = 2u * kExpertWBytes + (gather ? 0u : 128u * static_cast<uint32_t>(t.n));
-      for (int kb = 0; kb < p.num_kb; ++kb) {
+      for (int kb = kr.begin; kb < kr.end; ++kb) {
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.empty_bar[s]), phase ^ 1u, abort_flag));
         if (!ok) break;
         const uint32_t w_dst = smem + s * stage_bytes, x_dst = w_dst + kExpertWBytes;
-        const uint32_t full = map_to_cta(smem_u32(&sh.full_bar[s]), 0u);
+        const uint32_t full = map_to_cta(smem_u32(&sh.full_bar[s]), leader_rank);
         if (leader) {
           if (rank == 0) mbar_arrive_expect_tx(smem_u32(&sh.full_bar[s]), bytes);
           if constexpr (kSwiglu)
@@ -463,7 +488,7 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
       const uint32_t idesc = umma_idesc_bf16_f32(256, static_cast<uint32_t>(t.n)), a = used & 1u, acc = tmem + a * kExpertTileN;
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.acc_empty[a]), ((used >> 1) & 1u) ^ 1u, abort_flag));
       if (!ok) break;
-      for (int kb = 0; kb < p.num_kb; ++kb) {
+      for (int kb = kr.begin; kb < kr.end; ++kb) {
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.full_bar[s]), phase, abort_flag));
         if (!ok) break;
         tcgen05_fence_after();
@@ -472,9 +497,9 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
         if (leader) {
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk)                 // 32 bytes of K each
-            umma_bf16<2>(acc, adesc + 2u * kk, bdesc + 2u * kk, idesc, (kk != 0 || kb != 0) ? 1u : 0u);
-          umma_commit_pair(smem_u32(&sh.empty_bar[s]), 0u);
-          if (kb == p.num_kb - 1) umma_commit_pair(smem_u32(&sh.acc_full[a]), 0u);
+            umma_bf16<2>(acc, adesc + 2u * kk, bdesc + 2u * kk, idesc, (kk != 0 || kb != kr.begin) ? 1u : 0u);
+          umma_commit_pair(smem_u32(&sh.empty_bar[s]), cluster_rank);
+          if (kb == kr.end - 1) umma_commit_pair(smem_u32(&sh.acc_full[a]), cluster_rank);
         }
         __syncwarp();
         if (++s == stages) { s = 0; phase ^= 1u; }
@@ -482,10 +507,10 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
       ++used;
     }
   } else if (warp == 2 && gather) {
-    pass_on_rows(p, total, first, stride, stages, sh.x_bar, abort_flag, [&](uint32_t s) { mbar_arrive_pair(smem_u32(&sh.full_bar[s]), 0u); });
+    pass_on_rows(kr, total, first, stride, stages, sh.x_bar, abort_flag, [&](uint32_t s) { mbar_arrive_pair(smem_u32(&sh.full_bar[s]), leader_rank); });
   } else if (warp >= kExpertFirstGatherWarp) {
     if (gather)
-      gather_rows(p, total, first, stride, smem + kExpertWBytes, stages, stage_bytes, sh.empty_bar, sh.x_bar, abort_flag,
+      gather_rows(p, kr, total, first, stride, smem + kExpertWBytes, stages, stage_bytes, sh.empty_bar, sh.x_bar, abort_flag,
                                                     [&](int g, int row0, int32_t (&r)[kGatherRows]) {
         const ExpertTile t = expert_tile<kExpertTileN>(sh.tiles, p, g, slot);
 #pragma unroll
@@ -502,7 +527,7 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
     constexpr int kUnits = kSwiglu ? 2 : 4;              // of 16 bytes per row of a warp's results
     const int unit = lane % kUnits;
     uint32_t used = 0;
-    bool ok = true;
+    bool ok = true, met = false;
     for (int g = first; g < total && ok; g += stride) {
       const ExpertTile t = expert_tile<kExpertTileN>(sh.tiles, p, g, slot);
       const int column = (kSwiglu ? t.m * 128 + rank * 64 + quarter * 16 : t.m * 256 + rank * 128 + quarter * 32) + unit * 8;
@@ -510,11 +535,43 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.acc_full[a]), (used >> 1) & 1u, abort_flag));
       if (!ok) break;
       tcgen05_fence_after();
+      // split: chunk c / 32 of the tile lies at [chunk][quarter][vector of 4][lane] of the block's ring
+      const uint32_t parts = smem + static_cast<uint32_t>(quarter * 4096 + lane * 16);
+      if constexpr (kSplit) {
+        for (int c = 32 * half; c < t.n; c += 64) {
+          float u[16], l[16];
+          tmem_ld_16x256b(lanes + a * kExpertTileN + c, u);
+          tmem_ld_16x256b(lanes + (16u << 16) + a * kExpertTileN + c, l);
+          tmem_ld_wait();
+#pragma unroll
+          for (int v = 0; v < 8; ++v) {
+            const float* f = v < 4 ? u + 4 * v : l + 4 * (v - 4);
+            st_shared_v4(parts + 512u * c + 512u * v, __float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+          }
+        }
+        cluster_meet();
+        met = true;
+      }
       for (int c = 32 * half; c < t.n; c += 64) {
         float u[16], l[16];
-        tmem_ld_16x256b(lanes + a * kExpertTileN + c, u);
-        tmem_ld_16x256b(lanes + (16u << 16) + a * kExpertTileN + c, l);
-        tmem_ld_wait();
+        if constexpr (kSplit) {
+          if ((c >> 6) % p.pieces != piece) continue;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) u[i] = l[i] = 0.0f;
+          for (int from = 0; from < p.pieces; ++from) {
+            const uint32_t theirs = map_to_cta(parts + 512u * c, static_cast<uint32_t>(2 * from + rank));
+#pragma unroll
+            for (int v = 0; v < 8; ++v) {
+              const float4 w = ld_cluster_v4(theirs + 512u * v);
+              float* f = v < 4 ? u + 4 * v : l + 4 * (v - 4);
+              f[0] += w.x; f[1] += w.y; f[2] += w.z; f[3] += w.w;
+            }
+          }
+        } else {
+          tmem_ld_16x256b(lanes + a * kExpertTileN + c, u);
+          tmem_ld_16x256b(lanes + (16u << 16) + a * kExpertTileN + c, l);
+          tmem_ld_wait();
+        }
         if constexpr (kSwiglu) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) u[i] = swiglu(u[i], l[i]);
@@ -539,10 +596,14 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
       }
       tcgen05_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_pair(smem_u32(&sh.acc_empty[a]), 0u);
+      if (lane == 0) mbar_arrive_pair(smem_u32(&sh.acc_empty[a]), leader_rank);
       ++used;
     }
+    if constexpr (kSplit)
+      if (!met) cluster_meet();
   }
+  if constexpr (kSplit)
+    if (warp < kExpertFirstEpilogueWarp || warp >= kExpertFirstGatherWarp) cluster_meet();
 
   // ---------------------------------------------------------------- teardown
   tcgen05_fence_before();

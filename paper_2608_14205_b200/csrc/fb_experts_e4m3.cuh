@@ -91,10 +91,11 @@ __device__ __forceinline__ void fma_two(float& d0, float& d1, uint32_t a0, uint3
 // 660, with the read-out of TMEM 666, with the multiply-adds 805 - the chain wait, read, add, release of the eight warps, whose pipe
 // is 32 % busy.  Up projection with SwiGLU and quantised results, 256 experts of 7168 x 2048: 16384 tokens 4.3 ms (1796 TFLOP/s)
 // in short runs, 4.8 - 5.0 ms at 1000 W; 64 tokens 900 us, 6.6 TB/s (a copy: 6.53), and 935 - 970 us at 1000 W.
-template <bool kPair, bool kSwiglu, bool kQuantize>
+template <bool kPair, bool kSwiglu, bool kQuantize, bool kSplit>
 __global__ void __launch_bounds__(kExpertThreads, 1)
 fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                              const __grid_constant__ ExpertParams p) {
+  static_assert(!(kPair && kSplit), "a call of few tiles has no pairs");
   using L = ExpertE4m3Layout<kPair>;
   constexpr int kGroup = kPair ? 2 : 1;                  // blocks per tile
   extern __shared__ uint8_t smem_raw[];
@@ -102,6 +103,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
   const int lane = threadIdx.x & 31;
   const int rank = kPair ? static_cast<int>(cluster_ctarank()) : 0;
+  const int piece = kSplit ? static_cast<int>(cluster_ctarank()) : 0;
   const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
   volatile int* abort_flag = &sh.abort_flag;
   const bool gather = p.perm != nullptr;
@@ -136,7 +138,9 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
   uint32_t base;
   int slot = 0;                                          // of the warp's last tile
   const int total = expert_plan_tiles<L::kRows>(sh.tiles, p, base);
-  const int stride = static_cast<int>(gridDim.x) / kGroup, first = static_cast<int>(blockIdx.x) / kGroup;
+  const int sharers = kSplit ? p.pieces : kGroup;        // blocks per tile
+  const int stride = static_cast<int>(gridDim.x) / sharers, first = static_cast<int>(blockIdx.x) / sharers;
+  const KRange kr = kSplit ? k_range(p, piece) : KRange{0, p.num_kb};
 
   // Registers: 256 threads with 208 and 256 with 48 are the 512 x 128 of the launch.
   if (warp < kExpertFirstEpilogueWarp) {
@@ -152,7 +156,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
         // (loads without a row of the tile begin behind the last row of x and give zeros)
         const int i = rank * 128 + kTileLoadRows * lane, x_row = i < t.valid ? t.row + i : p.x_rows;
         const uint32_t bytes = kGroup * (L::kWBytes + (gather ? 0u : kE4m3XBytes));
-        for (int kb = 0; kb < p.num_kb; ++kb) {
+        for (int kb = kr.begin; kb < kr.end; ++kb) {
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.empty_bar[s]), phase ^ 1u, abort_flag));
           if (!ok) break;
           const uint32_t x_dst = smem + s * L::kStageBytes, w_dst = x_dst + kE4m3XBytes;
@@ -191,7 +195,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
       uint32_t s = 0, phase = 0, used = 0;               // accumulators begun
       bool ok = true;
       for (int g = first; g < total && ok; g += stride) {
-        for (int kb = 0; kb < p.num_kb; ++kb) {
+        for (int kb = kr.begin; kb < kr.end; ++kb) {
           const uint32_t a = used & 1u, acc = tmem + a * 256u;
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.full_bar[s]), phase, abort_flag));
           if (ok) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.acc_empty[a]), ((used >> 1) & 1u) ^ 1u, abort_flag));
@@ -216,7 +220,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
         }
       }
     } else if (warp == 2 && gather) {
-      pass_on_rows(p, total, first, stride, L::kStages, sh.x_bar, abort_flag, [&](uint32_t s) {
+      pass_on_rows(kr, total, first, stride, L::kStages, sh.x_bar, abort_flag, [&](uint32_t s) {
         if constexpr (kPair) mbar_arrive_pair(smem_u32(&sh.full_bar[s]), 0u);
         else mbar_arrive(smem_u32(&sh.full_bar[s]));
       });
@@ -224,7 +228,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
   } else if (warp >= kExpertFirstGatherWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (gather)
-      gather_rows(p, total, first, stride, smem, L::kStages, L::kStageBytes, sh.empty_bar, sh.x_bar, abort_flag,
+      gather_rows(p, kr, total, first, stride, smem, L::kStages, L::kStageBytes, sh.empty_bar, sh.x_bar, abort_flag,
                                                 [&](int g, int row0, int32_t (&r)[kGatherRows]) {
         const ExpertTile t = expert_tile<L::kRows>(sh.tiles, p, g, slot);
 #pragma unroll
@@ -238,7 +242,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
     const uint32_t from = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + 128u * half;
     const uint32_t staging = smem + L::kStagingAt + static_cast<uint32_t>(warp - kExpertFirstEpilogueWarp) * kE4m3WarpStaging;
     uint32_t used = 0, tiles_done = 0;
-    bool ok = true;
+    bool ok = true, met = false;
     // scales of the next k-blocks: this thread's row, and the blocks of W (gate and up; or this half's)
     const float *xs = nullptr, *w0 = nullptr, *w1 = nullptr;
     float v[kE4m3Ahead], a0[kE4m3Ahead], a1[kE4m3Ahead];
@@ -255,9 +259,10 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
       w0 = ws + static_cast<size_t>(kSwiglu ? t.m : min(2 * t.m + half, blocks - 1)) * p.scale_k;
       if constexpr (kSwiglu) w1 = w0 + static_cast<size_t>(blocks) * p.scale_k;
 #pragma unroll
-      for (int j = 0; j < kE4m3Ahead; ++j) load(j, j);
+      for (int j = 0; j < kE4m3Ahead; ++j) load(j, kr.begin + j);
     };
     // 64 bytes of each of the warp's 32 rows, from `value`, to column `first_byte` of out
+    const uint32_t owner_mask = kSplit ? static_cast<uint32_t>(p.pieces - 1) : 0u;      // split: the block that stores a row: its number modulo the pieces
     auto store = [&](const ExpertTile& t, size_t row_bytes, size_t first_byte, const uint32_t (&value)[16]) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -268,7 +273,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
       for (int i = 0; i < 4; ++i) {
         const int r = 8 * i + (lane >> 2), unit = lane & 3;
         const uint4 w = ld_shared_v4(staging + static_cast<uint32_t>(r * 64 + ((unit ^ ((r >> 1) & 3)) << 4)));
-        if (row0 + r < t.valid && first_byte + 16 * unit < row_bytes)
+        if (row0 + r < t.valid && first_byte + 16 * unit < row_bytes && (r & owner_mask) == static_cast<uint32_t>(piece))
           *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.out) + static_cast<size_t>(t.row + row0 + r) * row_bytes + first_byte + 16 * unit) = w;
       }
       __syncwarp();
@@ -291,14 +296,14 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
 #pragma unroll
       for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
       const bool any = row0 < t.valid;           // this warp has rows of x here
-      for (int kb = any ? p.num_kb : 0; kb < p.num_kb && ok; ++kb, ++used) {
+      for (int kb = any ? kr.end : kr.begin; kb < kr.end && ok; ++kb, ++used) {
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.acc_full[used & 1u]), (used >> 1) & 1u, abort_flag));
         if (ok) release(used & 1u);
       }
-      for (int kb0 = any ? 0 : p.num_kb; kb0 < p.num_kb && ok; kb0 += kE4m3Ahead) {
+      for (int kb0 = any ? kr.begin : kr.end; kb0 < kr.end && ok; kb0 += kE4m3Ahead) {
 #pragma unroll
         for (int j = 0; j < kE4m3Ahead; ++j) {
-          if (kb0 + j >= p.num_kb || !ok) break;
+          if (kb0 + j >= kr.end || !ok) break;
           const float s0 = v[j] * a0[j], s1 = kSwiglu ? v[j] * a1[j] : s0;
           load(j, kb0 + j + kE4m3Ahead);
           const uint32_t a = used & 1u;
@@ -333,6 +338,29 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
         }
       }
       if (!ok) break;
+      if constexpr (kSplit) {                            // [warp][vector of 4][lane] of the ring
+        const uint32_t parts = smem + static_cast<uint32_t>(warp - kExpertFirstEpilogueWarp) * 16384u + 16u * lane;
+        if (any) {
+#pragma unroll
+          for (int v = 0; v < 32; ++v)
+            st_shared_v4(parts + 512u * v, __float_as_uint(acc[4 * v]), __float_as_uint(acc[4 * v + 1]), __float_as_uint(acc[4 * v + 2]), __float_as_uint(acc[4 * v + 3]));
+        }
+        cluster_meet();
+        met = true;
+#pragma unroll
+        for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
+        if (any && (lane & owner_mask) == static_cast<uint32_t>(piece)) {
+          for (int from = 0; from < p.pieces; ++from) {
+            const uint32_t theirs = map_to_cta(parts, static_cast<uint32_t>(from));
+#pragma unroll
+            for (int v = 0; v < 32; ++v) {
+              const float4 w = ld_cluster_v4(theirs + 512u * v);
+              acc[4 * v] += w.x; acc[4 * v + 1] += w.y; acc[4 * v + 2] += w.z; acc[4 * v + 3] += w.w;
+            }
+          }
+        }
+        __syncwarp();
+      }
       const ExpertTile done = t;
       if (g + stride < total) {                          // the next tile's first scales arrive under the stores
         t = expert_tile<L::kRows>(sh.tiles, p, g + stride, slot);
@@ -367,19 +395,23 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
         if (!ok) break;
         top = fmaxf(top, tops[half ^ 1][quarter * 32 + lane]);
         const float inv = 448.0f / top;
-        if (half == 0 && row < done.valid) p.out_scale[static_cast<size_t>(done.row + row) * ((p.n_out + 127) / 128) + done.m] = top / 448.0f;
+        if (half == 0 && row < done.valid && (lane & owner_mask) == static_cast<uint32_t>(piece)) p.out_scale[static_cast<size_t>(done.row + row) * ((p.n_out + 127) / 128) + done.m] = top / 448.0f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) value[i] = pack_e4m3(acc[4 * i] * inv, acc[4 * i + 1] * inv, acc[4 * i + 2] * inv, acc[4 * i + 3] * inv);
         store(done, static_cast<size_t>(p.n_out), static_cast<size_t>(done.m * 128 + half * 64), value);
       }
       ++tiles_done;
     }
+    if constexpr (kSplit)
+      if (!met) cluster_meet();
   }
+  if constexpr (kSplit)
+    if (warp < kExpertFirstEpilogueWarp || warp >= kExpertFirstGatherWarp) cluster_meet();
 
   // ---------------------------------------------------------------- teardown
   tcgen05_fence_before();
   __syncthreads();
-  if constexpr (kPair) { cluster_arrive(); cluster_wait(); }              // nobody leaves while the partner may still signal it
+  if constexpr (kPair || kSplit) { cluster_arrive(); cluster_wait(); }    // nobody leaves while another may still signal it or read its sums
   if (threadIdx.x == 0 && sh.abort_flag) atomicCAS(p.status, 0, FB_ERR_TIMEOUT);
   if (warp == 1) {
     tcgen05_fence_after();

@@ -207,6 +207,29 @@ def test_many_rows_per_slot(form, counts, perm):
     ctx.close()
 
 
+@pytest.mark.parametrize("perm", [False, True])
+@pytest.mark.parametrize("counts", [[1], [40], [3, 0, 130], [256], [300, 20]], ids=str)
+@pytest.mark.parametrize("K", [512, 1040, 2064, 7168])
+@pytest.mark.parametrize("form", ["bf16", "bf16 swiglu", "e4m3", "e4m3 swiglu", "quantized"])
+def test_few_tiles_share_their_k_range(form, K, counts, perm):
+    # so few tiles that clusters share them: pieces of equal and of different length
+    e4m3, swiglu = form != "bf16" and form != "bf16 swiglu", form not in ("bf16", "e4m3")
+    ctx = make_ctx(k=2)
+    c = Case(counts, K, 320, e4m3, swiglu, perm, seed=K, whole=not swiglu)
+    got, scale = c.run(ctx, quantize=form == "quantized")
+    want, err = c.expected()
+    if not swiglu:
+        assert torch.equal(got, want.float().bfloat16())
+    elif scale is None:
+        assert ((got.double() - want).abs() <= err + (want.abs() + err) * 2.0 ** -8 + 2.0 ** -133).all()
+    else:
+        s = spread(scale, c.P, c.n_out, 1)
+        assert ((got.double() * s - want).abs() <= err + (want.abs() + err) * (2.0 ** -4 + 2.0 ** -20) + s * 2.0 ** -10).all()
+    again, _ = c.run(ctx, quantize=form == "quantized")
+    assert torch.equal(got.view(torch.uint8), again.view(torch.uint8))
+    ctx.close()
+
+
 @pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
 @pytest.mark.parametrize("perm", [False, True])
 def test_256_slots_and_one_token(e4m3, perm):
