@@ -1248,12 +1248,17 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   if (!ok) return FB_ERR_CUDA;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return FB_ERR_CUDA;
-  // Few tiles: clusters of up to 8 blocks share them (see KRange), as many pieces as leave each four k-blocks.
+  // Few tiles: clusters of up to 8 blocks share them (see KRange) where that saves each block 12 k-blocks of e4m3 (0.39 us each)
+  // or 16 of bf16 (0.2 us); meeting and adding up cost 2 - 4 us.  One matrix for 2 x 2048 results, whole and shared, us (K 2048,
+  // 3584, 7168): e4m3, 1 row 11.8 9.3, 16.5 10.6, 27.3 13.5; 64 rows 12.3 12.6, 17.2 13.9, 28.5 17.3; 300 rows (two pieces)
+  // 13.2 15.1, 17.9 17.8, 29.3 24.1.  bf16, 1 row 11.5 9.8, 16.1 12.1, 26.9 17.5; 300 rows 13.5 14.3, 18.3 16.8, 29.4 23.0.
   const int blocks_per_piece = pair ? 2 : 1;
   p.pieces = 1;
   if (!e4m3 || !pair)
     for (int pieces = 8 / blocks_per_piece; pieces > 1 && p.pieces == 1; pieces /= 2)
-      if (tiles <= ctx->max_clusters[pieces * blocks_per_piece / 2] && p.num_kb >= 4 * pieces) p.pieces = pieces;
+      if (tiles <= ctx->max_clusters[pieces * blocks_per_piece / 2] && p.num_kb >= 4 * pieces &&
+          p.num_kb - p.num_kb / pieces >= (e4m3 ? 12 : 16))
+        p.pieces = pieces;
   const bool split = p.pieces > 1;
   const ExpertKernel kernel = expert_kernel(e4m3, pair, split, swiglu, out_scale != nullptr);
   const int64_t at_once = split ? tiles : pair ? ctx->max_clusters[1] : ctx->n_sm, workers = tiles < at_once ? tiles : at_once;

@@ -73,7 +73,7 @@ struct ExpertParams {
 
 // Split launches.  A call with fewer tiles than the GPU has blocks (or pairs) for is latency: one tile's k-blocks one after the
 // other.  There a cluster shares the tile, each block (pair) a range of K; the partial sums go through the rings, which
-// are done with by then, and are added up in the order of the pieces by the block that stores the result.
+// are done with by then, and are added up in the order of the pieces by the block that stores the result.  (When: fb_expert_matmul.)
 struct KRange {
   int begin, end;                  // k-blocks
 };

@@ -262,7 +262,6 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
       for (int j = 0; j < kE4m3Ahead; ++j) load(j, kr.begin + j);
     };
     // 64 bytes of each of the warp's 32 rows, from `value`, to column `first_byte` of out
-    const uint32_t owner_mask = kSplit ? static_cast<uint32_t>(p.pieces - 1) : 0u;      // split: the block that stores a row: its number modulo the pieces
     auto store = [&](const ExpertTile& t, size_t row_bytes, size_t first_byte, const uint32_t (&value)[16]) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -273,7 +272,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
       for (int i = 0; i < 4; ++i) {
         const int r = 8 * i + (lane >> 2), unit = lane & 3;
         const uint4 w = ld_shared_v4(staging + static_cast<uint32_t>(r * 64 + ((unit ^ ((r >> 1) & 3)) << 4)));
-        if (row0 + r < t.valid && first_byte + 16 * unit < row_bytes && (r & owner_mask) == static_cast<uint32_t>(piece))
+        if (row0 + r < t.valid && first_byte + 16 * unit < row_bytes)
           *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.out) + static_cast<size_t>(t.row + row0 + r) * row_bytes + first_byte + 16 * unit) = w;
       }
       __syncwarp();
@@ -338,28 +337,82 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
         }
       }
       if (!ok) break;
-      if constexpr (kSplit) {                            // [warp][vector of 4][lane] of the ring
-        const uint32_t parts = smem + static_cast<uint32_t>(warp - kExpertFirstEpilogueWarp) * 16384u + 16u * lane;
+      if constexpr (kSplit) {                            // (a split launch has one tile per cluster)
+        // The sums of row `lane` lie at [warp][vector v of 4 columns][lane] of the ring.  A block adds up 32 / pieces rows of each
+        // quarter; in a warp `pieces` lanes share such a row, each `share` vectors of its results (SwiGLU: gate and up of them).
+        constexpr uint32_t kVector = 512 + 16;           // (the pad keeps the sharers of a row in different banks)
+        const uint32_t parts = smem + static_cast<uint32_t>(warp - kExpertFirstEpilogueWarp) * 32u * kVector;
         if (any) {
 #pragma unroll
           for (int v = 0; v < 32; ++v)
-            st_shared_v4(parts + 512u * v, __float_as_uint(acc[4 * v]), __float_as_uint(acc[4 * v + 1]), __float_as_uint(acc[4 * v + 2]), __float_as_uint(acc[4 * v + 3]));
+            st_shared_v4(parts + kVector * v + 16u * lane, __float_as_uint(acc[4 * v]), __float_as_uint(acc[4 * v + 1]),
+                         __float_as_uint(acc[4 * v + 2]), __float_as_uint(acc[4 * v + 3]));
         }
         cluster_meet();
         met = true;
+        constexpr int kVectors = kSwiglu ? 16 : 32;      // of results in this half of the columns
+        const int rows = 32 / p.pieces, mine = piece * rows + lane % rows, share = kVectors / p.pieces, v0 = lane / rows * share;
+        const bool stored = row0 + mine < t.valid;
+        float a[kVectors / 2][4], b[kSwiglu ? kVectors / 2 : 1][4];
 #pragma unroll
-        for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
-        if (any && (lane & owner_mask) == static_cast<uint32_t>(piece)) {
+        for (int i = 0; i < kVectors / 2; ++i)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) { a[i][c] = 0.0f; if constexpr (kSwiglu) b[i][c] = 0.0f; }
+        if (stored) {
           for (int from = 0; from < p.pieces; ++from) {
-            const uint32_t theirs = map_to_cta(parts, static_cast<uint32_t>(from));
+            const uint32_t theirs = map_to_cta(parts, static_cast<uint32_t>(from)) + 16u * mine;
 #pragma unroll
-            for (int v = 0; v < 32; ++v) {
-              const float4 w = ld_cluster_v4(theirs + 512u * v);
-              acc[4 * v] += w.x; acc[4 * v + 1] += w.y; acc[4 * v + 2] += w.z; acc[4 * v + 3] += w.w;
+            for (int i = 0; i < kVectors / 2; ++i) {
+              if (i < share) {
+                const int q = v0 + i, v = kSwiglu ? (q >> 2) * 8 + (q & 3) : q;
+                const float4 x = ld_cluster_v4(theirs + kVector * v);
+                a[i][0] += x.x; a[i][1] += x.y; a[i][2] += x.z; a[i][3] += x.w;
+                if constexpr (kSwiglu) {
+                  const float4 y = ld_cluster_v4(theirs + kVector * (v + 4));
+                  b[i][0] += y.x; b[i][1] += y.y; b[i][2] += y.z; b[i][3] += y.w;
+                }
+              }
             }
           }
         }
-        __syncwarp();
+        if constexpr (kSwiglu) {
+#pragma unroll
+          for (int i = 0; i < kVectors / 2; ++i)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) a[i][c] = swiglu(a[i][c], b[i][c]);
+        }
+        const size_t at = static_cast<size_t>(t.row + row0 + mine);
+        const int column = t.m * (kSwiglu ? 128 : 256) + half * 4 * kVectors + 4 * v0;
+        float inv = 0.0f;
+        if constexpr (kQuantize) {
+          float top = 0x1p-100f;
+#pragma unroll
+          for (int i = 0; i < kVectors / 2; ++i)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) top = fmaxf(top, fabsf(a[i][c]));      // (zeros where i >= share)
+          for (int d = rows; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+          if (lane < rows) sh.top[0][half][quarter * 32 + lane] = top;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&sh.top_bar[quarter]));
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.top_bar[quarter]), 0u, abort_flag));
+          if (!ok) break;
+          top = fmaxf(top, sh.top[0][half ^ 1][quarter * 32 + lane % rows]);
+          inv = 448.0f / top;
+          if (stored && half == 0 && lane < rows) p.out_scale[at * ((p.n_out + 127) / 128) + t.m] = top / 448.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < kVectors / 2; ++i) {
+          const int c = column + 4 * i;
+          if (i < share && stored && c < p.n_out) {
+            if constexpr (kQuantize)
+              *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(p.out) + at * p.n_out + c) =
+                  pack_e4m3(a[i][0] * inv, a[i][1] * inv, a[i][2] * inv, a[i][3] * inv);
+            else
+              *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + at * p.n_out + c) =
+                  make_uint2(pack_bf16(a[i][0], a[i][1]), pack_bf16(a[i][2], a[i][3]));
+          }
+        }
+        break;
       }
       const ExpertTile done = t;
       if (g + stride < total) {                          // the next tile's first scales arrive under the stores
@@ -395,7 +448,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
         if (!ok) break;
         top = fmaxf(top, tops[half ^ 1][quarter * 32 + lane]);
         const float inv = 448.0f / top;
-        if (half == 0 && row < done.valid && (lane & owner_mask) == static_cast<uint32_t>(piece)) p.out_scale[static_cast<size_t>(done.row + row) * ((p.n_out + 127) / 128) + done.m] = top / 448.0f;
+        if (half == 0 && row < done.valid) p.out_scale[static_cast<size_t>(done.row + row) * ((p.n_out + 127) / 128) + done.m] = top / 448.0f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) value[i] = pack_e4m3(acc[4 * i] * inv, acc[4 * i + 1] * inv, acc[4 * i + 2] * inv, acc[4 * i + 3] * inv);
         store(done, static_cast<size_t>(p.n_out), static_cast<size_t>(done.m * 128 + half * 64), value);
