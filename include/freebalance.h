@@ -423,8 +423,8 @@ fb_status fb_apply_swaps_staged(fb_ctx* ctx, void* slot_weights, uint64_t expert
  *   out[t] = sum over j of topk_w[t][j] * y[inv_perm[t k + j]]   fb_combine
  * Weights are bf16, or e4m3 with a scale for each block of 128 x 128; the rows that meet e4m3 weights are e4m3 with a
  * scale for each 128 columns (fb_quantize_rows; the SwiGLU product can hand out such rows itself).  Forward only: router
- * and experts are frozen here.  A row's result does not depend on the rows beside it, nor on its position, and equal
- * calls give equal bits.
+ * and experts are frozen here.  Equal calls give equal bits, and in calls of the same sizes (rows, slots, matrices) a
+ * row's result depends neither on the rows beside it nor on its position; other sizes may add a row's sums in another order.
  * All three run on ctx's device, allocate nothing, use no scratch of the context (calls may overlap on any streams) and
  * may be captured (tensor maps travel with the launch).  Sums, maxima and scales are formed in 32 bits.  Errors:
  * FB_ERR_INVALID_ARG, FB_ERR_UNSUPPORTED_SHAPE (a limit below, or sizes whose launch would pass 2^31 blocks),

@@ -49,7 +49,8 @@ constexpr int kExpertTileM = 256;                       // rows of W per pair
 constexpr int kExpertTileN = 256;                       // rows of x per tile at most
 constexpr int kExpertStepN = 32;                        // (the MMA of a pair takes N in steps of 32)
 constexpr uint32_t kExpertWBytes = 128 * 128;           // 128 rows of W, 128 bytes each
-constexpr int kBand = 8;                                // tiles of x that share a walk over W
+constexpr int kBand = 8;                                // tiles of x that share a walk over W (4, 8, 16, 64: 5.62, 5.64, 5.72, 5.94 ms for
+                                                        // 131072 tokens of 128 experts; 16384 and fewer: no difference)
 
 struct ExpertParams {
   const uint32_t* slot_offsets;    // [n_slots + 1] or NULL (one slot of `rows` rows)
