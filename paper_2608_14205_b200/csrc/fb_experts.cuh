@@ -109,6 +109,7 @@ struct ExpertShared {
   uint64_t full_bar[kExpertStages], empty_bar[kExpertStages];
   uint64_t x_bar[kExpertStages];                        // this block's gathered rows have arrived
   uint64_t acc_full[2], acc_empty[2];                   // per set of 256 columns
+  uint64_t rows_bar[2];                                 // SwiGLU, per half of the warps: 32 rows of results are staged
   uint32_t tmem_base;
   int32_t abort_flag;
   ExpertTiles tiles;
@@ -306,11 +307,12 @@ __device__ __forceinline__ int expert_x_row(const ExpertParams& p, uint32_t base
 
 template <bool kSwiglu>
 struct ExpertLayout {
-  // rows of 16 (SwiGLU) or 32 numbers with a pad that keeps eight rows in different banks
-  static constexpr int kRowBytes = kSwiglu ? 48 : 80;
-  static constexpr int kWarpStaging = 32 * kRowBytes;
+  // Rows with a pad that keeps eight of them in different banks.  SwiGLU: the 64 numbers of a block's part of a row, 32 rows, in
+  // two buffers for each half of the warps; else the 32 numbers of a warp, 32 rows for each warp.
+  static constexpr int kRowBytes = kSwiglu ? 144 : 80;
+  static constexpr int kBuffer = 32 * kRowBytes;
   static constexpr uint32_t kStagingAt = kExpertRingBytes;
-  static constexpr uint32_t kDynamic = kStagingAt + kExpertEpilogueWarps * kWarpStaging + 1024;
+  static constexpr uint32_t kDynamic = kStagingAt + (kSwiglu ? 4 : kExpertEpilogueWarps) * kBuffer + 1024;
 };
 
 // The gather warps' part of a kernel: for every k-block of every tile, rows_of(g, row0, r) gives the row numbers of this
@@ -418,6 +420,7 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
     for (int a = 0; a < 2; ++a) {
       mbar_init(smem_u32(&sh.acc_full[a]), 1);
       mbar_init(smem_u32(&sh.acc_empty[a]), 2 * kExpertEpilogueWarps);
+      mbar_init(smem_u32(&sh.rows_bar[a]), kExpertEpilogueWarps / 2);
     }
     fence_mbar_init();
     if (!gather) prefetch_tensormap(&map_x);           // (a gather has none)
@@ -522,16 +525,19 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
     // -------------------------------------------------------------- results
     const int quarter = warp & 3, half = (warp - kExpertFirstEpilogueWarp) >> 2;     // TMEM lanes; chunks of 32 columns half, half + 2, ..
     const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
-    const uint32_t staging = smem + L::kStagingAt + static_cast<uint32_t>(warp - kExpertFirstEpilogueWarp) * L::kWarpStaging;
-    // matrix i of an stmatrix: columns 8 (g + i / 2) .., rows 8 (i % 2) ..
-    const uint32_t to = staging + static_cast<uint32_t>((8 * ((lane >> 4) & 1) + (lane & 7)) * L::kRowBytes + ((lane >> 3) & 1) * 16);
-    constexpr int kUnits = kSwiglu ? 2 : 4;              // of 16 bytes per row of a warp's results
+    const uint32_t staging = smem + L::kStagingAt + static_cast<uint32_t>((kSwiglu ? 2 * half : warp - kExpertFirstEpilogueWarp) * L::kBuffer);
+    // matrix i of an stmatrix: columns 8 (g + i / 2) .., rows 8 (i % 2) ..; SwiGLU: 16 of the row's 64 numbers are this warp's
+    const uint32_t to = staging + static_cast<uint32_t>((8 * ((lane >> 4) & 1) + (lane & 7)) * L::kRowBytes + ((lane >> 3) & 1) * 16 + (kSwiglu ? 32 * quarter : 0));
+    // what a warp stores: 16 bytes per lane; SwiGLU: 8 of the 32 rows, whole lines (131072 tokens: 5.75 -> 5.67 ms; a warp's own 16
+    // numbers are 32 bytes of a line); else its own 32 numbers of each row
+    constexpr int kUnits = kSwiglu ? 8 : 4;              // lanes per row
     const int unit = lane % kUnits;
+    uint32_t passes = 0;
     uint32_t used = 0;
     bool ok = true, met = false;
     for (int g = first; g < total && ok; g += stride) {
       const ExpertTile t = expert_tile<kExpertTileN>(sh.tiles, p, g, slot);
-      const int column = (kSwiglu ? t.m * 128 + rank * 64 + quarter * 16 : t.m * 256 + rank * 128 + quarter * 32) + unit * 8;
+      const int column = (kSwiglu ? t.m * 128 + rank * 64 : t.m * 256 + rank * 128 + quarter * 32) + unit * 8;
       const uint32_t a = used & 1u;
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.acc_full[a]), (used >> 1) & 1u, abort_flag));
       if (!ok) break;
@@ -577,24 +583,34 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
 #pragma unroll
           for (int i = 0; i < 16; ++i) u[i] = swiglu(u[i], l[i]);
         }
+        const uint32_t buffer = kSwiglu ? (passes & 1u) * L::kBuffer : 0u;
 #pragma unroll
         for (int q = 0; q < 4; q += 2) {
-          stmatrix_x4_trans(to + 8u * q * L::kRowBytes, pack_bf16(u[4 * q], u[4 * q + 1]), pack_bf16(u[4 * q + 2], u[4 * q + 3]),
+          stmatrix_x4_trans(to + buffer + 8u * q * L::kRowBytes, pack_bf16(u[4 * q], u[4 * q + 1]), pack_bf16(u[4 * q + 2], u[4 * q + 3]),
                             pack_bf16(u[4 * q + 4], u[4 * q + 5]), pack_bf16(u[4 * q + 6], u[4 * q + 7]));
           if constexpr (!kSwiglu)
             stmatrix_x4_trans(to + 8u * q * L::kRowBytes + 32u, pack_bf16(l[4 * q], l[4 * q + 1]), pack_bf16(l[4 * q + 2], l[4 * q + 3]),
                               pack_bf16(l[4 * q + 4], l[4 * q + 5]), pack_bf16(l[4 * q + 6], l[4 * q + 7]));
         }
         __syncwarp();
+        if constexpr (kSwiglu) {
+          // the four quarters' numbers; who fills a buffer again has seen all of them at the barrier of the other one
+          if (lane == 0) mbar_arrive(smem_u32(&sh.rows_bar[half]));
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.rows_bar[half]), passes & 1u, abort_flag));
+          if (!ok) break;
+          ++passes;
+        }
+        constexpr int kStores = kSwiglu ? 2 : 4;
 #pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-          const int r = i * (32 / kUnits) + lane / kUnits;
-          const uint4 v = ld_shared_v4(staging + static_cast<uint32_t>(r * L::kRowBytes + unit * 16));
+        for (int i = 0; i < kStores; ++i) {
+          const int r = (kSwiglu ? 8 * quarter : 0) + i * (32 / kUnits) + lane / kUnits;
+          const uint4 v = ld_shared_v4(staging + buffer + static_cast<uint32_t>(r * L::kRowBytes + unit * 16));
           if (c + r < t.valid && column < p.n_out)
             *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + static_cast<size_t>(t.row + c + r) * p.n_out + column) = v;
         }
         __syncwarp();
       }
+      if (!ok) break;
       tcgen05_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_pair(smem_u32(&sh.acc_empty[a]), leader_rank);
