@@ -468,7 +468,8 @@ fb_status fb_quantize_rows(fb_ctx* ctx, const void* x, int64_t rows, int32_t n, 
  *                 slot_offsets + s0 and its own matrices.  NULL: one slot (n_slots 1) that has all rows
  *   perm          dev i32 [x_rows k], indexed by p, or NULL
  *   rows          rows that out holds; slot_offsets[n_slots] - slot_offsets[0] may be less, and rows of out behind it
- *                 are left as they are.  Slots may be empty.
+ *                 are left as they are.  Slots may be empty.  (The kernel is chosen by rows and n_slots: pass the step's
+ *                 own T k, not a capacity.)
  *   out           dev bf16 [rows][n_out], n_out = n (n / 2 with FB_ACT_SWIGLU), rounded once from 32 bits (silu(g) is
  *                 taken as 0 for g below -87); with out_scale (e4m3 and FB_ACT_SWIGLU only) e4m3 [rows][n_out], quantised as by fb_quantize_rows from the 32-bit values
  *   out_scale     dev f32 [rows][ceil(n_out / 128)] or NULL
