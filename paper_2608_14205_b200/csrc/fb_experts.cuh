@@ -372,6 +372,17 @@ __device__ __forceinline__ void gather_rows(const ExpertParams& p, KRange k, int
   cp_async_wait_all();
 }
 
+// The loading warp's end: every stage is free again.  A commit of the MMAs arrives at the barriers of both blocks of a pair, in no
+// order with the other commit behind the same MMAs, so the results' barrier says nothing about these arrivals: without this wait
+// a block could leave while one is on its way to its shared memory.  (A stage never used passes at once.)
+__device__ __forceinline__ bool take_back_stages(uint64_t* empty_bar, uint32_t s, uint32_t phase, uint32_t stages, volatile int* abort_flag) {
+  for (uint32_t i = 0; i < stages; ++i) {
+    if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&empty_bar[s]), phase ^ 1u, abort_flag))) return false;
+    if (++s == stages) { s = 0; phase ^= 1u; }
+  }
+  return true;
+}
+
 // One warp's part: gathered rows that have arrived are made visible to the tensor core and reported.
 template <typename Arrive>
 __device__ __forceinline__ void pass_on_rows(KRange k, int total, int first, int stride, uint32_t stages, uint64_t* x_bar,
@@ -477,6 +488,7 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
         if (++s == stages) { s = 0; phase ^= 1u; }
       }
     }
+    if (ok) ok = take_back_stages(sh.empty_bar, s, phase, stages, abort_flag);
     if (!ok && rank == 0) {                              // given up: the copies under way end before the block does
       volatile int never = 0;
       for (uint32_t f = fills > stages ? fills - stages : 0; f < fills; ++f)

@@ -183,6 +183,7 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
           if (++s == L::kStages) { s = 0; phase ^= 1u; }
         }
       }
+      if (ok) ok = take_back_stages(sh.empty_bar, s, phase, L::kStages, abort_flag);
       if (!ok && rank == 0) {                            // given up: the copies under way end before the block does
         volatile int never = 0;
         for (uint32_t f = fills > L::kStages ? fills - L::kStages : 0; f < fills; ++f)
