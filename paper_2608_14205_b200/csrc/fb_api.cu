@@ -149,6 +149,19 @@ fb_status check_config(const fb_config& c) {
   return FB_OK;
 }
 
+// A tensor map in the 128-byte swizzle, zeros outside; ctx's device is the current one.  The encoding is a call of the driver's, which wants
+// a context of the host thread: one that has made no other CUDA call has none until cudaSetDevice gives it one.
+bool encode_map(const fb_ctx* ctx, CUtensorMap* map, CUtensorMapDataType type, int dims, const void* ptr, const cuuint64_t* size,
+                const cuuint64_t* stride, const cuuint32_t* box) {
+  const cuuint32_t one[5] = {1, 1, 1, 1, 1};
+  auto encode = [&] {
+    return ctx->encode(map, type, static_cast<cuuint32_t>(dims), const_cast<void*>(ptr), size, stride, box, one,
+                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  return encode() || (cudaSetDevice(ctx->device) == cudaSuccess && encode());
+}
+
 fb_status make_map(fb_ctx* ctx, MapEntry* cache, int* next, const void* ptr, int64_t rows, uint32_t box_rows,
                    const CUtensorMap** out) {
   for (int i = 0; i < kMapCache; ++i)
@@ -162,11 +175,11 @@ fb_status make_map(fb_ctx* ctx, MapEntry* cache, int* next, const void* ptr, int
   const cuuint64_t gdim[2] = {static_cast<cuuint64_t>(ctx->cfg.d), static_cast<cuuint64_t>(rows)};
   const cuuint64_t gstride[1] = {static_cast<cuuint64_t>(ctx->cfg.d) * 2};
   const cuuint32_t box[2] = {static_cast<cuuint32_t>(fb::kBlockK), box_rows};
-  const cuuint32_t estride[2] = {1, 1};
-  const CUresult r = ctx->encode(&e.map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), gdim, gstride,
-                                 box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) { e.ptr = nullptr; e.rows = -1; return FB_ERR_CUDA; }
+  if (!encode_map(ctx, &e.map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, ptr, gdim, gstride, box)) {
+    e.ptr = nullptr;
+    e.rows = -1;
+    return FB_ERR_CUDA;
+  }
   e.ptr = ptr;
   e.rows = rows;
   e.box_rows = box_rows;
@@ -1217,14 +1230,10 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   p.max_tiles = rows / (pair ? 256 : 128) + (m->n_slots < rows ? m->n_slots : rows);
   const int64_t tiles = p.max_tiles * static_cast<int64_t>(p.m_blocks);
   if (tiles > (int64_t{1} << 30)) return FB_ERR_UNSUPPORTED_SHAPE;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return FB_ERR_CUDA;
   CUtensorMap map_x, map_w;
   const CUtensorMapDataType type = e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-  auto encode = [&](CUtensorMap* map, int dims, const void* ptr, const cuuint64_t* size, const cuuint64_t* stride, const cuuint32_t* box) {
-    const cuuint32_t one[5] = {1, 1, 1, 1, 1};
-    return ctx->encode(map, type, static_cast<cuuint32_t>(dims), const_cast<void*>(ptr), size, stride, box, one,
-                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-  };
   const cuuint64_t K = static_cast<cuuint64_t>(m->K), E = static_cast<cuuint64_t>(m->n_slots);
   const cuuint32_t width = static_cast<cuuint32_t>(step);
   // one slot has no stride: any value that the map takes
@@ -1233,21 +1242,19 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   if (perm == nullptr) {
     const cuuint64_t size[2] = {K, static_cast<cuuint64_t>(x_rows)}, stride[1] = {row_bytes};
     const cuuint32_t box[2] = {width, fb::kTileLoadRows};
-    ok = encode(&map_x, 2, x, size, stride, box);
+    ok = encode_map(ctx, &map_x, type, 2, x, size, stride, box);
   }
   if (swiglu) {                                                    // 16 rows of gate, 16 of up, ..
     const cuuint64_t size[5] = {K, 16, 2, static_cast<cuuint64_t>(p.n_out / 16), E};
     const cuuint64_t stride[4] = {row_bytes, row_bytes * p.n_out, row_bytes * 16, slot_bytes};
     const cuuint32_t box[5] = {width, 16, 2, pair ? 4u : 8u, 1};
-    ok = ok && encode(&map_w, 5, m->w, size, stride, box);
+    ok = ok && encode_map(ctx, &map_w, type, 5, m->w, size, stride, box);
   } else {
     const cuuint64_t size[3] = {K, static_cast<cuuint64_t>(m->n), E}, stride[2] = {row_bytes, slot_bytes};
     const cuuint32_t box[3] = {width, pair ? 128u : 256u, 1};
-    ok = ok && encode(&map_w, 3, m->w, size, stride, box);
+    ok = ok && encode_map(ctx, &map_w, type, 3, m->w, size, stride, box);
   }
   if (!ok) return FB_ERR_CUDA;
-  DeviceGuard guard(ctx->device);
-  if (!guard.ok) return FB_ERR_CUDA;
   // Few tiles: clusters of up to 8 blocks share them (see KRange) where that saves each block 12 k-blocks of e4m3 (0.39 us each)
   // or 16 of bf16 (0.2 us); meeting and adding up cost 2 - 4 us.  One matrix for 2 x 2048 results, whole and shared, us (K 2048,
   // 3584, 7168): e4m3, 1 row 11.8 9.3, 16.5 10.6, 27.3 13.5; 64 rows 12.3 12.6, 17.2 13.9, 28.5 17.3; 300 rows (two pieces)
