@@ -427,8 +427,8 @@ fb_status fb_apply_swaps_staged(fb_ctx* ctx, void* slot_weights, uint64_t expert
  * row's result depends neither on the rows beside it nor on its position; other sizes may add a row's sums in another order.
  * All three run on ctx's device, allocate nothing, use no scratch of the context (calls may overlap on any streams) and
  * may be captured (tensor maps travel with the launch).  Sums, maxima and scales are formed in 32 bits.  Errors:
- * FB_ERR_INVALID_ARG, FB_ERR_UNSUPPORTED_SHAPE (a limit below, or sizes whose launch would pass 2^31 blocks),
- * FB_ERR_CUDA; device status as named at each call. */
+ * FB_ERR_INVALID_ARG, FB_ERR_UNSUPPORTED_SHAPE (a limit below; n, K, rows or x_rows of a product, n of the other two
+ * above 2^31 - 1024; sizes whose launch would pass 2^31 blocks), FB_ERR_CUDA; device status as named at each call. */
 
 typedef enum {
   FB_ACT_NONE = 0,

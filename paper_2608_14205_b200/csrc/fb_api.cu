@@ -552,6 +552,9 @@ ExpertKernel expert_kernel(bool e4m3, bool pair, bool split, bool swiglu, bool q
 // Constant data inside the library image, so the calibration allocates nothing.
 __device__ const int32_t g_calibration_plan[8] = {0, 1, 0, 1, 0, 1, 1, 0};
 
+// Numbers of a row, rows: the largest that a tile's length can be added to in 32 bits.
+constexpr int32_t kMostLength = INT32_MAX - 1023;
+
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 template <typename Tp>
@@ -1173,6 +1176,7 @@ fb_status fb_quantize_rows(fb_ctx* ctx, const void* x, int64_t rows, int32_t n, 
   if (!ctx || rows < 0 || n <= 0 || n % 16 != 0) return FB_ERR_INVALID_ARG;
   if (rows == 0) return FB_OK;
   if (!x || !q || !scale || !aligned16(x) || !aligned16(q)) return FB_ERR_INVALID_ARG;
+  if (n > kMostLength) return FB_ERR_UNSUPPORTED_SHAPE;
   const int blocks_k = (n + 127) / 128;
   const int64_t per_block = fb::kQuantizeThreads / 16 * fb::kQuantizeUnroll;
   if (rows > (int64_t{1} << 31) * per_block / blocks_k - per_block) return FB_ERR_UNSUPPORTED_SHAPE;
@@ -1192,6 +1196,7 @@ fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* m, const void* x
   if (m->act != FB_ACT_NONE && m->act != FB_ACT_SWIGLU) return FB_ERR_INVALID_ARG;
   const bool e4m3 = m->dtype == FB_DTYPE_E4M3, swiglu = m->act == FB_ACT_SWIGLU;
   if (m->n_slots <= 0 || m->n <= 0 || m->K <= 0 || !m->w || !aligned16(m->w) || m->slot_bytes % 16 != 0) return FB_ERR_INVALID_ARG;
+  if (m->n > kMostLength || m->K > kMostLength || rows > kMostLength || x_rows > kMostLength) return FB_ERR_UNSUPPORTED_SHAPE;
   if (m->n_slots > FB_MAX_EXPERTS || m->K % (e4m3 ? 16 : 8) != 0 || m->n % (swiglu ? 32 : 8) != 0) return FB_ERR_UNSUPPORTED_SHAPE;
   const uint64_t row_bytes = static_cast<uint64_t>(m->K) * (e4m3 ? 1 : 2);
   if (row_bytes >= (uint64_t{1} << 31) || m->slot_bytes >= (uint64_t{1} << 40) || row_bytes * static_cast<uint64_t>(m->n) >= (uint64_t{1} << 40)) return FB_ERR_UNSUPPORTED_SHAPE;
@@ -1294,6 +1299,7 @@ fb_status fb_combine(fb_ctx* ctx, const void* rows, const float* w, const int32_
   if (!ctx || T < 0 || n <= 0 || n % 8 != 0) return FB_ERR_INVALID_ARG;
   if (T == 0) return FB_OK;
   if (!rows || !w || !inv_perm || !out || !aligned16(rows) || !aligned16(out) || !aligned16(addend)) return FB_ERR_INVALID_ARG;
+  if (n > kMostLength) return FB_ERR_UNSUPPORTED_SHAPE;
   const int k = ctx->cfg.k, pieces = (n / 8 + fb::kCombineThreads - 1) / fb::kCombineThreads;
   if (static_cast<int64_t>(T) * (pieces > k ? pieces : k) >= (int64_t{1} << 31)) return FB_ERR_UNSUPPORTED_SHAPE;
   using CombineFn = void (*)(const __nv_bfloat16*, const float*, const int32_t*, int, int, int, const __nv_bfloat16*, __nv_bfloat16*, int32_t*);
