@@ -242,6 +242,8 @@ FB_ACT_NONE, FB_ACT_SWIGLU = 0, 1
 
 
 _EXPERT_DTYPES = {torch.bfloat16: (FB_DTYPE_BF16, 2), torch.float8_e4m3fn: (FB_DTYPE_E4M3, 1)}
+_EXPERT_ROWS = {FB_DTYPE_BF16: torch.bfloat16, FB_DTYPE_E4M3: torch.float8_e4m3fn}
+_INDEX_DTYPES = (torch.int32, torch.uint32)
 
 
 def make_expert_matrix(w: torch.Tensor, scale: Optional[torch.Tensor] = None, act: int = FB_ACT_NONE) -> FbExpertMatrix:
@@ -412,10 +414,25 @@ class Context:
             _check(st, "fb_quantize_rows")
 
     def fb_expert_matmul(self, matrix, x, x_scale, slot_offsets, perm, rows, out, out_scale=None, stream=None):
-        """x: [x_rows, K] of the matrix's type; out: [rows, n_out] bf16, or e4m3 with out_scale."""
+        """x: [x_rows, K] of the matrix's type; out: [rows, n_out] bf16, or e4m3 with out_scale; slot_offsets (one more than slots)
+        and perm (an entry for every position that the offsets name): 32-bit integers."""
         x_rows, K = x.shape
         assert K == matrix.K, "rows of x: as long as the matrix's"
-        assert out is None or out.element_size() == (2 if out_scale is None else 1), "bf16 results, e4m3 ones with out_scale"
+        of = _EXPERT_ROWS.get(matrix.dtype)
+        assert of is None or x.dtype == of, "x: of the matrix's type"
+        assert slot_offsets is None or slot_offsets.dtype in _INDEX_DTYPES, "slot_offsets: 32-bit integers"
+        assert perm is None or perm.dtype in _INDEX_DTYPES, "perm: 32-bit integers"
+        assert out is None or out.dtype == (torch.bfloat16 if out_scale is None else torch.float8_e4m3fn), "bf16 results, e4m3 ones with out_scale"
+        assert x_scale is None or x_scale.dtype == torch.float32, "x_scale: float32"
+        n_out = matrix.n // 2 if matrix.act == FB_ACT_SWIGLU else matrix.n
+        short = ((x_scale is not None and x_scale.numel() < x_rows * ((K + 127) // 128))
+                 or (slot_offsets is not None and slot_offsets.numel() <= matrix.n_slots)
+                 or (out is not None and out.numel() < rows * n_out))
+        if out_scale is not None:
+            assert out_scale.dtype == torch.float32, "out_scale: float32"
+            short = short or out_scale.numel() < rows * ((n_out + 127) // 128)
+        if short:
+            raise FbError(FB_ERR_INVALID_ARG, "fb_expert_matmul: a tensor is too short")
         st = lib().fb_expert_matmul(self._h, ctypes.byref(matrix), _ptr(x), _ptr(x_scale), x_rows, _ptr(slot_offsets), _ptr(perm), rows,
                                     _ptr(out), _ptr(out_scale), _stream(stream))
         if st:
