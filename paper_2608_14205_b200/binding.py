@@ -439,6 +439,17 @@ class Context:
             _check(st, "fb_expert_matmul")
 
     def fb_combine(self, rows, w, inv_perm, T, n, addend, out, stream=None):
+        """rows: bf16 [T k, n]; w: float32 [T, k]; inv_perm: 32-bit integers [T k]; addend, out: bf16 [T, n]."""
+        bf16 = torch.bfloat16
+        assert (rows is None or rows.dtype == bf16) and (out is None or out.dtype == bf16), "bf16 rows"
+        assert addend is None or addend.dtype == bf16, "addend: bf16"
+        assert w is None or w.dtype == torch.float32, "w: float32"
+        assert inv_perm is None or inv_perm.dtype in _INDEX_DTYPES, "inv_perm: 32-bit integers"
+        chosen = T * self.cfg.k
+        if chosen < 2**31 and ((w is not None and w.numel() < chosen) or (inv_perm is not None and inv_perm.numel() < chosen)
+                               or (rows is not None and rows.numel() < chosen * n) or (out is not None and out.numel() < T * n)
+                               or (addend is not None and addend.numel() < T * n)):
+            raise FbError(FB_ERR_INVALID_ARG, "fb_combine: a tensor is too short")       # (more positions: the library refuses them)
         st = lib().fb_combine(self._h, _ptr(rows), _ptr(w), _ptr(inv_perm), T, n, _ptr(addend), _ptr(out), _stream(stream))
         if st:
             _check(st, "fb_combine")

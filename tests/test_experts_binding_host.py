@@ -78,3 +78,33 @@ def test_products_with_too_few_elements(ctx, name, e4m3, quantize):
     with pytest.raises(B.FbError) as e:
         ctx.fb_expert_matmul(**a)
     assert e.value.status == B.FB_ERR_INVALID_ARG and ctx.calls == []
+
+
+def sum_of_rows():
+    """Good arguments: 4 tokens, k = 2."""
+    return dict(rows=bf(8, 64), w=f32(4, 2), inv_perm=i32(8), T=4, n=64, addend=bf(4, 64), out=bf(4, 64))
+
+
+def test_good_combinations_reach_the_library(ctx):
+    ctx.fb_combine(**sum_of_rows())
+    ctx.fb_combine(**{**sum_of_rows(), "addend": None, "T": 3})
+    assert ctx.calls == ["fb_combine"] * 2
+
+
+@pytest.mark.parametrize("name,dtype", [("rows", torch.float16), ("rows", torch.float32), ("w", torch.bfloat16), ("w", torch.float64),
+                                        ("inv_perm", torch.int64), ("addend", torch.float16), ("out", torch.float16), ("out", torch.float32)], ids=str)
+def test_combinations_with_tensors_of_another_type(ctx, name, dtype):
+    a = sum_of_rows()
+    a[name] = a[name].to(dtype)
+    with pytest.raises(AssertionError):
+        ctx.fb_combine(**a)
+    assert ctx.calls == []
+
+
+@pytest.mark.parametrize("name", ["rows", "w", "inv_perm", "addend", "out"])
+def test_combinations_with_too_few_elements(ctx, name):
+    a = sum_of_rows()
+    a[name] = a[name].reshape(-1)[:-1]
+    with pytest.raises(B.FbError) as e:
+        ctx.fb_combine(**a)
+    assert e.value.status == B.FB_ERR_INVALID_ARG and ctx.calls == []
