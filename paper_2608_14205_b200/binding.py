@@ -408,7 +408,11 @@ class Context:
                                         *[_ptr(o) for o in outs], _stream(stream)), "fb_layer_step_host")
 
     def fb_quantize_rows(self, x, rows, n, q, scale, stream=None):
-        assert x.dtype == torch.bfloat16 and scale.dtype == torch.float32
+        """x: bf16 [rows, n]; q: e4m3 [rows, n]; scale: float32 [rows, ceil(n / 128)]."""
+        assert x.dtype == torch.bfloat16 and scale.dtype == torch.float32 and (q is None or q.dtype == torch.float8_e4m3fn)
+        blocks = rows * ((n + 127) // 128)
+        if blocks < 2**37 and (x.numel() < rows * n or (q is not None and q.numel() < rows * n) or scale.numel() < blocks):
+            raise FbError(FB_ERR_INVALID_ARG, "fb_quantize_rows: a tensor is too short")       # (more blocks: the library refuses them)
         st = lib().fb_quantize_rows(self._h, _ptr(x), rows, n, _ptr(q), _ptr(scale), _stream(stream))
         if st:
             _check(st, "fb_quantize_rows")

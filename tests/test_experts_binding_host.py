@@ -108,3 +108,34 @@ def test_combinations_with_too_few_elements(ctx, name):
     with pytest.raises(B.FbError) as e:
         ctx.fb_combine(**a)
     assert e.value.status == B.FB_ERR_INVALID_ARG and ctx.calls == []
+
+
+def rows_to_quantize():
+    """Good arguments: 4 rows of 144 numbers."""
+    return dict(x=bf(4, 144), rows=4, n=144, q=f8(4, 144), scale=f32(4, 2))
+
+
+def test_good_quantisations_reach_the_library(ctx):
+    ctx.fb_quantize_rows(**rows_to_quantize())
+    ctx.fb_quantize_rows(**{**rows_to_quantize(), "rows": 3})
+    ctx.fb_quantize_rows(**{**rows_to_quantize(), "rows": 2**40, "n": 7168})      # the library's own refusal
+    assert ctx.calls == ["fb_quantize_rows"] * 3
+
+
+@pytest.mark.parametrize("name,dtype", [("x", torch.float16), ("x", torch.float32), ("q", torch.bfloat16), ("q", torch.float8_e5m2),
+                                        ("scale", torch.bfloat16)], ids=str)
+def test_quantisations_with_tensors_of_another_type(ctx, name, dtype):
+    a = rows_to_quantize()
+    a[name] = a[name].to(torch.float32).to(dtype)
+    with pytest.raises(AssertionError):
+        ctx.fb_quantize_rows(**a)
+    assert ctx.calls == []
+
+
+@pytest.mark.parametrize("name", ["x", "q", "scale"])
+def test_quantisations_with_too_few_elements(ctx, name):
+    a = rows_to_quantize()
+    a[name] = a[name].reshape(-1)[:-1]
+    with pytest.raises(B.FbError) as e:
+        ctx.fb_quantize_rows(**a)
+    assert e.value.status == B.FB_ERR_INVALID_ARG and ctx.calls == []
