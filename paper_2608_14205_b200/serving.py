@@ -109,11 +109,11 @@ class ServingLoop:
             report = dict(cos_hidden=cos_hidden, cos_logits=cos_logits, hit_rate=hits / (T * k) if T * k else 1.0)
         # the plan is committed: the buffer that held the old placement receives the next one
         self.placement[layer], self._spare = pi_new, pi
-        return dict(out=o, pi_old=pi, pi_new=pi_new, **report)
+        return dict(out=o, pi_old=pi, pi_new=pi_new, T=T, **report)
 
     def experts_step(self, r: dict, H: torch.Tensor, experts: X.SlotExperts, addend: Optional[torch.Tensor] = None,
                      stream=None) -> torch.Tensor:
-        """The output of the layer whose step `r` layer_step returned last: [T, d], overwritten by the next call.
+        """The output of the layer whose step `r` layer_step returned last, for that step's H: [T, d], overwritten by the next call.
 
         `experts` are the layer's images in the slots of the placement before that step; the plan's swaps are applied to
         them first (stage 3 of the method), so the images are those of r["pi_new"] afterwards.  A step's swaps are
@@ -121,7 +121,8 @@ class ServingLoop:
         if torch._C._cuda_getDevice() != self.device:
             with torch.cuda.device(self.device):
                 return self.experts_step(r, H, experts, addend, stream)
-        T, o, k = H.shape[0], self.out, self.wl.k
+        T, o, k = r["T"], self.out, self.wl.k
+        assert H.shape[0] == T, "the hidden states of another batch than the step's"
         buf = self._x
         if buf is None or buf.key != (experts.d, experts.inter, experts.e4m3, self.T_max, k):
             buf = self._x = X.ExpertBuffers(experts, self.T_max, k)

@@ -1,0 +1,61 @@
+"""ServingLoop.experts_step: what it refuses, which buffers it keeps and how its stream is ordered, with stand-ins for the
+loop's parts and for torch's device calls: nothing is launched."""
+import types
+
+import pytest
+import torch
+
+from paper_2608_14205_b200 import experts as X
+from paper_2608_14205_b200 import serving as S
+
+T_MAX, D, K = 16, 32, 2
+
+
+class Experts:
+    """Images of which only the sizes are looked at."""
+
+    def __init__(self, inter=16, e4m3=False):
+        self.d, self.inter, self.e4m3, self.dtype = D, inter, e4m3, torch.bfloat16
+        self.images = torch.zeros(1)
+        self.swapped = 0
+
+    def apply_swaps(self, *a, stream=None):
+        self.swapped += 1
+
+
+class Buffers:
+    def __init__(self, experts, tokens, k):
+        self.key = (experts.d, experts.inter, experts.e4m3, tokens, k)
+
+
+@pytest.fixture
+def loop(monkeypatch):
+    """A loop of one layer; loop.ran lists the calls of run_experts as (buffers, H, T)."""
+    ran = []
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(S.X, "ExpertBuffers", Buffers)
+    monkeypatch.setattr(S.X, "run_experts", lambda ctx, experts, buf, H, T, *a: ran.append((buf, H, T)) or H)
+    l = S.ServingLoop.__new__(S.ServingLoop)
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)
+    l.wl, l.T_max, l.device, l.dev = types.SimpleNamespace(d=D, E=4, k=K), T_MAX, 0, torch.device("cpu")
+    l.ctx = types.SimpleNamespace(fb_layer_step=lambda *a: None)
+    l.out = {name: i32(8) for name in ("counts", "swaps", "n_swaps", "load_before", "load_after", "ids", "w", "slot_offsets",
+                                       "rank_offsets", "perm", "inv_perm", "rank_load")}
+    l.placement, l._spare, l._q, l._x, l._buffers = {}, i32(4), None, None, {}
+    l.ran = ran
+    return l
+
+
+def rows(T):
+    return torch.zeros(T, D, dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("tokens", [1, 7, 9, T_MAX, T_MAX + 1])
+def test_hidden_states_of_another_batch_are_refused(loop, tokens):
+    x = Experts()
+    r = loop.layer_step(0, None, rows(8), rows(8), None)
+    with pytest.raises(AssertionError):
+        loop.experts_step(r, rows(tokens), x)
+    assert x.swapped == 0 and loop.ran == []
+    loop.experts_step(r, rows(8), x)
+    assert x.swapped == 1 and [t for _, _, t in loop.ran] == [8]
