@@ -122,6 +122,7 @@ class ServingLoop:
             with torch.cuda.device(self.device):
                 return self.experts_step(r, H, experts, addend, stream)
         T, o, k = r["T"], self.out, self.wl.k
+        assert r["pi_old"] is self._spare, "a later step has overwritten this one's index and plan"
         assert H.shape[0] == T, "the hidden states of another batch than the step's"
         buf = self._x
         if buf is None or buf.key != (experts.d, experts.inter, experts.e4m3, self.T_max, k):

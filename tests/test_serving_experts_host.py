@@ -59,3 +59,14 @@ def test_hidden_states_of_another_batch_are_refused(loop, tokens):
     assert x.swapped == 0 and loop.ran == []
     loop.experts_step(r, rows(8), x)
     assert x.swapped == 1 and [t for _, _, t in loop.ran] == [8]
+
+
+def test_a_step_that_a_later_one_has_overwritten_is_refused(loop):
+    x = Experts()
+    first = loop.layer_step(0, None, rows(8), rows(8), None)
+    second = loop.layer_step(1, None, rows(8), rows(8), None)
+    with pytest.raises(AssertionError):
+        loop.experts_step(first, rows(8), x)
+    assert x.swapped == 0 and loop.ran == []
+    loop.experts_step(second, rows(8), x)
+    assert x.swapped == 1
