@@ -85,7 +85,6 @@ class ExpertBuffers:
 
     def __init__(self, experts: SlotExperts, tokens: int, k: int):
         dev, d, inter, rows = experts.images.device, experts.d, experts.inter, max(1, tokens * k)
-        self.key = (d, inter, experts.e4m3, tokens, k)
         self.hidden = torch.empty(rows, inter, dtype=experts.dtype, device=dev)
         self.rows = torch.empty(rows, d, dtype=torch.bfloat16, device=dev)
         self.out = torch.empty(max(1, tokens), d, dtype=torch.bfloat16, device=dev)

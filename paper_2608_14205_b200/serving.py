@@ -55,7 +55,8 @@ class ServingLoop:
         self.placement: Dict[int, torch.Tensor] = {}      # layer -> expert_to_slot in force
         self._spare = i32(E)                              # receives the next placement
         self._q: Optional[dict] = None                    # quality-mode buffers, allocated on first use
-        self._x: Optional[X.ExpertBuffers] = None         # buffers of experts_step, allocated on first use
+        self._x: Optional[X.ExpertBuffers] = None         # buffers of the last experts_step
+        self._buffers: Dict[tuple, X.ExpertBuffers] = {}  # of every size of experts so far: kept, work on them may be under way
 
     def close(self):
         self.ctx.close()
@@ -124,9 +125,10 @@ class ServingLoop:
         T, o, k = r["T"], self.out, self.wl.k
         assert r["pi_old"] is self._spare, "a later step has overwritten this one's index and plan"
         assert H.shape[0] == T, "the hidden states of another batch than the step's"
-        buf = self._x
-        if buf is None or buf.key != (experts.d, experts.inter, experts.e4m3, self.T_max, k):
-            buf = self._x = X.ExpertBuffers(experts, self.T_max, k)
+        key = (experts.d, experts.inter, experts.e4m3, self.T_max, k)
+        if key not in self._buffers:
+            self._buffers[key] = X.ExpertBuffers(experts, self.T_max, k)
+        buf = self._x = self._buffers[key]
         experts.apply_swaps(r["pi_old"], o["swaps"], o["n_swaps"], o["swaps"].numel() // 4, stream=stream)
         return X.run_experts(self.ctx, experts, buf, H, T, k, o["w"], o["slot_offsets"], o["perm"], o["inv_perm"], addend,
                              stream)

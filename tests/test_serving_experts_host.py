@@ -25,7 +25,7 @@ class Experts:
 
 class Buffers:
     def __init__(self, experts, tokens, k):
-        self.key = (experts.d, experts.inter, experts.e4m3, tokens, k)
+        self.size = (experts.inter, experts.e4m3, tokens, k)
 
 
 @pytest.fixture
@@ -70,3 +70,13 @@ def test_a_step_that_a_later_one_has_overwritten_is_refused(loop):
     assert x.swapped == 0 and loop.ran == []
     loop.experts_step(second, rows(8), x)
     assert x.swapped == 1
+
+
+def test_buffers_stay_when_experts_of_another_size_are_used(loop):
+    # work on them may be under way on any stream, or captured in a graph that will be replayed
+    narrow, wide = Experts(16), Experts(64, e4m3=True)
+    for x in (narrow, wide, narrow, Experts(16), wide):
+        loop.experts_step(loop.layer_step(0, None, rows(8), rows(8), None), rows(8), x)
+        assert loop._x is loop.ran[-1][0]
+    a, b, c, d, e = (buf for buf, _, _ in loop.ran)
+    assert a is c is d and b is e and a.size == (16, False, T_MAX, K) and b.size == (64, True, T_MAX, K)
