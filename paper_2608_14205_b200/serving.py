@@ -118,7 +118,9 @@ class ServingLoop:
 
         `experts` are the layer's images in the slots of the placement before that step; the plan's swaps are applied to
         them first (stage 3 of the method), so the images are those of r["pi_new"] afterwards.  A step's swaps are
-        applied once: call this once per layer_step.  addend [T, d]: a shared expert's output or a residual."""
+        applied once: call this once per layer_step.  addend [T, d]: a shared expert's output or a residual.
+        stream: where the work runs; it begins behind what the current stream has so far (the step's index and plan), and the
+        current stream goes on behind it (the next step overwrites them)."""
         if torch._C._cuda_getDevice() != self.device:
             with torch.cuda.device(self.device):
                 return self.experts_step(r, H, experts, addend, stream)
@@ -129,9 +131,19 @@ class ServingLoop:
         if key not in self._buffers:
             self._buffers[key] = X.ExpertBuffers(experts, self.T_max, k)
         buf = self._x = self._buffers[key]
-        experts.apply_swaps(r["pi_old"], o["swaps"], o["n_swaps"], o["swaps"].numel() // 4, stream=stream)
-        return X.run_experts(self.ctx, experts, buf, H, T, k, o["w"], o["slot_offsets"], o["perm"], o["inv_perm"], addend,
-                             stream)
+        current = torch.cuda.current_stream(self.dev) if stream is not None else None
+        side = torch.cuda.ExternalStream(stream, device=self.dev) if isinstance(stream, int) else stream
+        if side is not None and side.cuda_stream == current.cuda_stream:
+            side = None
+        if side is not None:
+            side.wait_stream(current)
+        try:
+            experts.apply_swaps(r["pi_old"], o["swaps"], o["n_swaps"], o["swaps"].numel() // 4, stream=stream)
+            return X.run_experts(self.ctx, experts, buf, H, T, k, o["w"], o["slot_offsets"], o["perm"], o["inv_perm"], addend,
+                                 stream)
+        finally:
+            if side is not None:
+                current.wait_stream(side)
 
     def realised_loads(self, r: dict, budget: B.FbBudget):
         """Realised per-expert counts of the last layer step and the rank loads they give under the

@@ -80,3 +80,41 @@ def test_buffers_stay_when_experts_of_another_size_are_used(loop):
         assert loop._x is loop.ran[-1][0]
     a, b, c, d, e = (buf for buf, _, _ in loop.ran)
     assert a is c is d and b is e and a.size == (16, False, T_MAX, K) and b.size == (64, True, T_MAX, K)
+
+
+class Stream:
+    """Notes in `log` what waits for what."""
+
+    def __init__(self, name, handle, log):
+        self.name, self.cuda_stream, self.log = name, handle, log
+
+    def wait_stream(self, other):
+        self.log.append(f"{self.name} waits for {other.name}")
+
+
+@pytest.mark.parametrize("given", ["none", "current", "side", "side by handle"])
+@pytest.mark.parametrize("fails", [False, True], ids=["runs", "fails"])
+def test_a_stream_begins_behind_the_current_one_which_goes_on_behind_it(loop, monkeypatch, given, fails):
+    # layer_step writes index and plan on the current stream, the next one overwrites them there
+    log = []
+    current, side = Stream("current", 7, log), Stream("side", 9, log)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: current)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: {7: current, 9: side}[handle])
+    x = Experts()
+    x.apply_swaps = lambda *a, stream=None: log.append(("swaps", stream))
+
+    def run(ctx, experts, buf, H, T, *a):
+        log.append(("products", a[-1]))
+        if fails:
+            raise RuntimeError("refused")
+
+    monkeypatch.setattr(S.X, "run_experts", run)
+    stream = {"none": None, "current": current, "side": side, "side by handle": 9}[given]
+    r = loop.layer_step(0, None, rows(8), rows(8), None)
+    if fails:
+        with pytest.raises(RuntimeError):
+            loop.experts_step(r, rows(8), x, stream=stream)
+    else:
+        loop.experts_step(r, rows(8), x, stream=stream)
+    work = [("swaps", stream), ("products", stream)]
+    assert log == (["side waits for current", *work, "current waits for side"] if given.startswith("side") else work)
