@@ -299,7 +299,7 @@ __device__ __forceinline__ int expert_x_row(const ExpertParams& p, uint32_t base
   int x = t.row + min(i, t.valid - 1);                   // counted from slot_offsets[0]; no branch: a thread's loads go out together
   if (p.perm != nullptr) {
     const int32_t entry = p.perm[static_cast<size_t>(base) + x];
-    x = entry < 0 ? -1 : static_cast<int>(static_cast<uint32_t>(entry) / static_cast<uint32_t>(p.k));      // (-1 / k would be row 0)
+    x = static_cast<int>(static_cast<uint32_t>(entry) / static_cast<uint32_t>(p.k)) | entry >> 31;      // (a negative entry: -1, not row 0)
   }
   if (static_cast<unsigned>(x) >= static_cast<unsigned>(p.x_rows)) {
     atomicCAS(p.status, 0, FB_ERR_RANGE);
