@@ -44,11 +44,11 @@ constexpr int kGatherRows = 8;                          // rows per thread: 128 
 constexpr int kTileLoadRows = 16;                       // rows of x per TMA load
 constexpr int kNoRow = -2, kZeroRow = -1;
 constexpr uint32_t kExpertRingBytes = 6 * 32768;         // stages of 128 rows of W and as many of x as the largest tile has
-constexpr int kExpertStages = 12;                       // at most
 constexpr int kExpertTileM = 256;                       // rows of W per pair
 constexpr int kExpertTileN = 256;                       // rows of x per tile at most
 constexpr int kExpertStepN = 32;                        // (the MMA of a pair takes N in steps of 32)
 constexpr uint32_t kExpertWBytes = 128 * 128;           // 128 rows of W, 128 bytes each
+constexpr int kExpertStages = kExpertRingBytes / (kExpertWBytes + 64 * kExpertStepN);      // of the smallest tile
 constexpr int kBand = 8;                                // tiles of x that share a walk over W (4, 8, 16, 64: 5.62, 5.64, 5.72, 5.94 ms for
                                                         // 131072 tokens of 128 experts; 16384 and fewer: no difference)
 
@@ -459,7 +459,7 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
   const KRange kr = kSplit ? k_range(p, piece) : KRange{0, p.num_kb};
   // Few rows per tile leave room for more stages: what is under way is W, and a launch of few tiles has few blocks to ask for it.
   const uint32_t stage_bytes = kExpertWBytes + 64u * static_cast<uint32_t>(max(sh.tiles.most, kExpertStepN));
-  const uint32_t stages = min(kExpertRingBytes / stage_bytes, static_cast<uint32_t>(kExpertStages));
+  const uint32_t stages = kExpertRingBytes / stage_bytes;      // (kExpertStages at most)
 
   if (warp == 0) {
     // -------------------------------------------------------------- TMA loads
