@@ -192,6 +192,16 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr()
 
 
+def _arg(t: Optional[torch.Tensor], dtypes: tuple, count: int, what: str) -> Optional[int]:
+    """The pointer of a tensor of one of these types with `count` elements at least (one pass over it: 0.1 us a tensor)."""
+    if t is None:
+        return None
+    assert t.dtype in dtypes and t.is_contiguous(), what
+    if t.numel() < count:
+        raise FbError(FB_ERR_INVALID_ARG, f"too few elements for {what}")
+    return t.data_ptr()
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:                   # torch's current stream without building a Stream object (3 us of a call's 14)
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) or None
@@ -242,8 +252,8 @@ FB_ACT_NONE, FB_ACT_SWIGLU = 0, 1
 
 
 _EXPERT_DTYPES = {torch.bfloat16: (FB_DTYPE_BF16, 2), torch.float8_e4m3fn: (FB_DTYPE_E4M3, 1)}
-_EXPERT_ROWS = {FB_DTYPE_BF16: torch.bfloat16, FB_DTYPE_E4M3: torch.float8_e4m3fn}
-_INDEX_DTYPES = (torch.int32, torch.uint32)
+_BF16, _F32, _E4M3, _INT32 = (torch.bfloat16,), (torch.float32,), (torch.float8_e4m3fn,), (torch.int32, torch.uint32)
+_EXPERT_ROWS = {FB_DTYPE_BF16: _BF16, FB_DTYPE_E4M3: _E4M3}
 
 
 def make_expert_matrix(w: torch.Tensor, scale: Optional[torch.Tensor] = None, act: int = FB_ACT_NONE) -> FbExpertMatrix:
@@ -341,7 +351,7 @@ class Context:
         self.cfg = FbConfig(T_max, d, E, k, R, gate, n_group, topk_group, renorm, route_scale)
         self._h = ctypes.c_void_p()
         _check(lib().fb_create(ctypes.byref(self._h), ctypes.byref(self.cfg), device), "fb_create")
-        self.device = device
+        self.device, self._k = device, k
 
     def close(self):
         if getattr(self, "_h", None) is not None and self._h:
@@ -409,11 +419,11 @@ class Context:
 
     def fb_quantize_rows(self, x, rows, n, q, scale, stream=None):
         """x: bf16 [rows, n]; q: e4m3 [rows, n]; scale: float32 [rows, ceil(n / 128)]."""
-        assert x.dtype == torch.bfloat16 and scale.dtype == torch.float32 and (q is None or q.dtype == torch.float8_e4m3fn)
-        blocks = rows * ((n + 127) // 128)
-        if blocks < 2**37 and (x.numel() < rows * n or (q is not None and q.numel() < rows * n) or scale.numel() < blocks):
-            raise FbError(FB_ERR_INVALID_ARG, "fb_quantize_rows: a tensor is too short")       # (more blocks: the library refuses them)
-        st = lib().fb_quantize_rows(self._h, _ptr(x), rows, n, _ptr(q), _ptr(scale), _stream(stream))
+        numbers, blocks = rows * n, rows * ((n + 127) // 128)
+        if blocks >= 2**37:                  # refused by the library whatever the tensors hold
+            numbers = blocks = 0
+        st = lib().fb_quantize_rows(self._h, _arg(x, _BF16, numbers, "x: bf16 [rows, n]"), rows, n, _arg(q, _E4M3, numbers, "q: e4m3 [rows, n]"),
+                                    _arg(scale, _F32, blocks, "scale: float32 [rows, ceil(n / 128)]"), _stream(stream))
         if st:
             _check(st, "fb_quantize_rows")
 
@@ -422,39 +432,25 @@ class Context:
         and perm (an entry for every position that the offsets name): 32-bit integers."""
         x_rows, K = x.shape
         assert K == matrix.K, "rows of x: as long as the matrix's"
-        of = _EXPERT_ROWS.get(matrix.dtype)
-        assert of is None or x.dtype == of, "x: of the matrix's type"
-        assert slot_offsets is None or slot_offsets.dtype in _INDEX_DTYPES, "slot_offsets: 32-bit integers"
-        assert perm is None or perm.dtype in _INDEX_DTYPES, "perm: 32-bit integers"
-        assert out is None or out.dtype == (torch.bfloat16 if out_scale is None else torch.float8_e4m3fn), "bf16 results, e4m3 ones with out_scale"
-        assert x_scale is None or x_scale.dtype == torch.float32, "x_scale: float32"
         n_out = matrix.n // 2 if matrix.act == FB_ACT_SWIGLU else matrix.n
-        short = ((x_scale is not None and x_scale.numel() < x_rows * ((K + 127) // 128))
-                 or (slot_offsets is not None and slot_offsets.numel() <= matrix.n_slots)
-                 or (out is not None and out.numel() < rows * n_out))
-        if out_scale is not None:
-            assert out_scale.dtype == torch.float32, "out_scale: float32"
-            short = short or out_scale.numel() < rows * ((n_out + 127) // 128)
-        if short:
-            raise FbError(FB_ERR_INVALID_ARG, "fb_expert_matmul: a tensor is too short")
-        st = lib().fb_expert_matmul(self._h, ctypes.byref(matrix), _ptr(x), _ptr(x_scale), x_rows, _ptr(slot_offsets), _ptr(perm), rows,
-                                    _ptr(out), _ptr(out_scale), _stream(stream))
+        x_at = _arg(x, _EXPERT_ROWS.get(matrix.dtype) or (x.dtype,), 0, "x: of the matrix's type")      # (another type: the library's refusal)
+        st = lib().fb_expert_matmul(
+            self._h, ctypes.byref(matrix), x_at, _arg(x_scale, _F32, x_rows * ((K + 127) // 128), "x_scale: float32 [x_rows, ceil(K / 128)]"),
+            x_rows, _arg(slot_offsets, _INT32, matrix.n_slots + 1, "slot_offsets: 32-bit integers [n_slots + 1]"),
+            _arg(perm, _INT32, 0, "perm: 32-bit integers"), rows,
+            _arg(out, _BF16 if out_scale is None else _E4M3, rows * n_out, "out: bf16 [rows, n_out], e4m3 with out_scale"),
+            _arg(out_scale, _F32, rows * ((n_out + 127) // 128), "out_scale: float32 [rows, ceil(n_out / 128)]"), _stream(stream))
         if st:
             _check(st, "fb_expert_matmul")
 
     def fb_combine(self, rows, w, inv_perm, T, n, addend, out, stream=None):
         """rows: bf16 [T k, n]; w: float32 [T, k]; inv_perm: 32-bit integers [T k]; addend, out: bf16 [T, n]."""
-        bf16 = torch.bfloat16
-        assert (rows is None or rows.dtype == bf16) and (out is None or out.dtype == bf16), "bf16 rows"
-        assert addend is None or addend.dtype == bf16, "addend: bf16"
-        assert w is None or w.dtype == torch.float32, "w: float32"
-        assert inv_perm is None or inv_perm.dtype in _INDEX_DTYPES, "inv_perm: 32-bit integers"
-        chosen = T * self.cfg.k
-        if chosen < 2**31 and ((w is not None and w.numel() < chosen) or (inv_perm is not None and inv_perm.numel() < chosen)
-                               or (rows is not None and rows.numel() < chosen * n) or (out is not None and out.numel() < T * n)
-                               or (addend is not None and addend.numel() < T * n)):
-            raise FbError(FB_ERR_INVALID_ARG, "fb_combine: a tensor is too short")       # (more positions: the library refuses them)
-        st = lib().fb_combine(self._h, _ptr(rows), _ptr(w), _ptr(inv_perm), T, n, _ptr(addend), _ptr(out), _stream(stream))
+        numbers, chosen = T * n, T * self._k
+        if chosen >= 2**31:                  # refused by the library whatever the tensors hold
+            numbers = chosen = 0
+        st = lib().fb_combine(self._h, _arg(rows, _BF16, chosen * n, "rows: bf16 [T k, n]"), _arg(w, _F32, chosen, "w: float32 [T, k]"),
+                              _arg(inv_perm, _INT32, chosen, "inv_perm: 32-bit integers [T k]"), T, n,
+                              _arg(addend, _BF16, numbers, "addend: bf16 [T, n]"), _arg(out, _BF16, numbers, "out: bf16 [T, n]"), _stream(stream))
         if st:
             _check(st, "fb_combine")
 

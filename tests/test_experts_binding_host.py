@@ -1,7 +1,5 @@
 """What the binding refuses before the library is called: tensors of another type or with too few elements, whose pointers alone
 the library could not tell from good ones.  A stand-in takes the library's place: nothing is launched."""
-import types
-
 import pytest
 import torch
 
@@ -27,8 +25,7 @@ def ctx(monkeypatch):
     monkeypatch.setattr(B, "_stream", lambda stream: None)
     monkeypatch.setattr(B, "_lib", None)
     c = B.Context.__new__(B.Context)
-    c._h, c.device, c.calls = None, 0, calls
-    c.cfg = types.SimpleNamespace(k=2)
+    c._h, c.device, c._k, c.calls = None, 0, 2, calls
     return c
 
 
