@@ -101,6 +101,7 @@ def run_experts(ctx: B.Context, experts: SlotExperts, buf: ExpertBuffers, H: tor
 
     Up projection with SwiGLU over the tokens' rows in dispatch order, down projection, combination: three launches,
     with e4m3 images four (the rows of H are quantised once per token; the up projection quantises its own results)."""
+    assert H.shape[1] == experts.d, "hidden states of another size than the experts'"
     rows = T * k
     out = buf.out[:T]
     x, x_scale, hidden_scale = H, None, None

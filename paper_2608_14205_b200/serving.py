@@ -126,6 +126,7 @@ class ServingLoop:
                 return self.experts_step(r, H, experts, addend, stream)
         T, o, k = r["T"], self.out, self.wl.k
         assert r["pi_old"] is self._spare, "a later step has overwritten this one's index and plan"
+        assert (experts.E, experts.d) == (self.wl.E, self.wl.d) and experts.images.device == self.dev, "images of another model or device"
         assert H.shape[0] == T, "the hidden states of another batch than the step's"
         key = (experts.d, experts.inter, experts.e4m3, self.T_max, k)
         if key not in self._buffers:

@@ -14,9 +14,9 @@ T_MAX, D, K = 16, 32, 2
 class Experts:
     """Images of which only the sizes are looked at."""
 
-    def __init__(self, inter=16, e4m3=False):
-        self.d, self.inter, self.e4m3, self.dtype = D, inter, e4m3, torch.bfloat16
-        self.images = torch.zeros(1)
+    def __init__(self, inter=16, e4m3=False, d=D, E=4, device="cpu"):
+        self.d, self.E, self.inter, self.e4m3, self.dtype = d, E, inter, e4m3, torch.bfloat16
+        self.images = torch.zeros(1, device=device)
         self.swapped = 0
 
     def apply_swaps(self, *a, stream=None):
@@ -118,3 +118,25 @@ def test_a_stream_begins_behind_the_current_one_which_goes_on_behind_it(loop, mo
         loop.experts_step(r, rows(8), x, stream=stream)
     work = [("swaps", stream), ("products", stream)]
     assert log == (["side waits for current", *work, "current waits for side"] if given.startswith("side") else work)
+
+
+@pytest.mark.parametrize("other", [dict(d=16), dict(d=64), dict(E=3), dict(E=5), dict(device="meta")], ids=str)
+def test_images_of_another_model_or_device_are_refused(loop, other):
+    x = Experts(e4m3=True, **other)
+    r = loop.layer_step(0, None, rows(8), rows(8), None)
+    with pytest.raises(AssertionError):
+        loop.experts_step(r, rows(8), x)
+    assert x.swapped == 0 and loop.ran == []
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [D - 16, D + 16])
+def test_rows_of_another_length_are_refused(e4m3, d):
+    x = X.SlotExperts.__new__(X.SlotExperts)
+    x.d, x.e4m3, x.up_matrix, x.down_matrix = d, e4m3, types.SimpleNamespace(K=d), None
+    made = []
+    ctx = types.SimpleNamespace(**{name: lambda *a, stream=None, name=name: made.append(name) for name in ("fb_quantize_rows", "fb_expert_matmul", "fb_combine")})
+    buf = types.SimpleNamespace(out=rows(8), x=rows(8), x_scale=rows(8), hidden=rows(16), hidden_scale=rows(16), rows=rows(16))
+    with pytest.raises(AssertionError):
+        X.run_experts(ctx, x, buf, rows(8), 8, K, None, None, None, None)
+    assert made == []
