@@ -471,10 +471,11 @@ fb_status fb_quantize_rows(fb_ctx* ctx, const void* x, int64_t rows, int32_t n, 
  *                 are left as they are.  Slots may be empty.  (The kernel is chosen by rows and n_slots: pass the step's
  *                 own T k, not a capacity.)
  *   out           dev bf16 [rows][n_out], n_out = n (n / 2 with FB_ACT_SWIGLU), rounded once from 32 bits (silu(g) is
- *                 taken as 0 for g below -87); with out_scale (e4m3 and FB_ACT_SWIGLU only) e4m3 [rows][n_out], quantised as by fb_quantize_rows from the 32-bit values
+ *                 taken as 0 for g below -87); with out_scale (e4m3 and FB_ACT_SWIGLU only) e4m3 [rows][n_out],
+ *                 quantised as by fb_quantize_rows from the 32-bit values
  *   out_scale     dev f32 [rows][ceil(n_out / 128)] or NULL
  * out overlaps no input.  One launch.  Device status FB_ERR_RANGE: offsets that do not rise, pass `rows` or
- * (with perm) x_rows k (that slot's rows are left out), an entry of perm outside x (row 0 is read instead). */
+ * (with perm) x_rows k (that slot's rows are left out), an entry of perm outside [0, x_rows k) (row 0 is read instead). */
 fb_status fb_expert_matmul(fb_ctx* ctx, const fb_expert_matrix* matrix, const void* x, const float* x_scale, int32_t x_rows,
                            const uint32_t* slot_offsets, const int32_t* perm, int32_t rows, void* out, float* out_scale,
                            fb_stream stream);

@@ -404,10 +404,11 @@ __device__ __forceinline__ void pass_on_rows(KRange k, int total, int first, int
 }
 
 // Large calls are bound by the tensor cores under the power limit: 131072 x 2048 with 128 experts of 768, up projection with
-// SwiGLU, 4.75 ms (1388 TFLOP/s) in short runs and 5.65 ms (1165) at 1000 W; one 8192 x 8192 x 8192 product 855 us there, cuBLAS
-// 860 - 900.  Ragged ones lose what small tiles cost (8192 tokens, slots of 150 - 2000 rows: 353 and 425 us, 1168 and 970).  Few rows
-// are bound by the stream of W: 40 tokens, down projection, 56.5 us, 6.2 TB/s of 6.5 measured; one token, 50 MB, 13.4 us, of
-// which 8.6 are the stream (96 SMs have tiles), the rest launch, offsets, row numbers and the way out one after the other.
+// SwiGLU, 4.75 ms (1388 TFLOP/s) in short runs and 5.57 - 5.88 ms (1184 - 1122) at 1000 W; one 8192 x 8192 x 8192 product 855 us there,
+// cuBLAS 860 - 900.  Ragged ones lose what small tiles and their fixed stride cost (8192 tokens, slots of 150 - 2000 rows: 353 us and
+// 418 - 449, 1168 and 987 - 918; the busiest pair has 9 - 11 % more columns than the mean).  Few rows are bound by the stream of W: 40
+// tokens, down projection, 56.5 us, 6.2 TB/s of 6.5 measured; one token, 50 MB, 13.4 us (13.7 where every pass reads other experts,
+// from HBM), of which 8.6 are the stream (96 SMs have tiles), the rest launch, offsets, row numbers and the way out one after the other.
 template <bool kSwiglu, bool kSplit>
 __global__ void __launch_bounds__(kExpertThreads, 1)
 fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
@@ -543,8 +544,8 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
     const uint32_t staging = smem + L::kStagingAt + static_cast<uint32_t>((kSwiglu ? 2 * half : warp - kExpertFirstEpilogueWarp) * L::kBuffer);
     // matrix i of an stmatrix: columns 8 (g + i / 2) .., rows 8 (i % 2) ..; SwiGLU: 16 of the row's 64 numbers are this warp's
     const uint32_t to = staging + static_cast<uint32_t>((8 * ((lane >> 4) & 1) + (lane & 7)) * L::kRowBytes + ((lane >> 3) & 1) * 16 + (kSwiglu ? 32 * quarter : 0));
-    // what a warp stores: 16 bytes per lane; SwiGLU: 8 of the 32 rows, whole lines (131072 tokens: 5.75 -> 5.67 ms; a warp's own 16
-    // numbers are 32 bytes of a line); else its own 32 numbers of each row
+    // what a warp stores: 16 bytes per lane; SwiGLU: 8 of the 32 rows, whole lines (131072 tokens: 5.75 -> 5.67 ms, in turn on one box;
+    // a warp's own 16 numbers are 32 bytes of a line); else its own 32 numbers of each row
     constexpr int kUnits = kSwiglu ? 8 : 4;              // lanes per row
     const int unit = lane % kUnits;
     uint32_t passes = 0;
@@ -650,7 +651,8 @@ fb_expert_matmul_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_
 
 // ---------------------------------------------------------------- rows to e4m3 with block scales
 // Half a warp per block of 128 columns: a = max(max |x|, 2^-100), s = a / 448, q = x * (448 / a) rounded to e4m3.
-// HBM bound: 3 bytes per number; 16384 x 7168 in 54.1 us, 6.58 TB/s (a copy: 6.53).  A thread has kQuantizeUnroll loads of 16 bytes, of consecutive blocks, under way together.
+// HBM bound: 3 bytes per number; 16384 x 7168 in 54.1 us in a graph, 6.58 TB/s (a copy: 6.53), 57 - 59 us in calls one by one.  A thread has
+// kQuantizeUnroll loads of 16 bytes, of consecutive blocks, under way together.
 constexpr int kQuantizeThreads = 256;
 constexpr int kQuantizeUnroll = 4;
 
@@ -708,7 +710,7 @@ fb_quantize_rows_kernel(const __nv_bfloat16* __restrict__ x, long long rows, int
 // ---------------------------------------------------------------- weighted sum of a token's rows
 // y[t] = sum over j of w[t][j] * rows[inv_perm[t k + j]] (+ addend[t]), j ascending, in 32 bits, rounded once.
 // HBM bound: k + 1 (+ 1) rows per token; a thread has its k loads of 16 bytes under way together.  16384 tokens of 8 rows of
-// 7168: 314.6 us, 6.72 TB/s (a copy: 6.53).
+// 7168: 314 - 318 us, 6.7 TB/s (a copy, half of whose bytes are written: 6.53).
 constexpr int kCombineThreads = 128;
 
 template <int kK>

@@ -90,7 +90,7 @@ __device__ __forceinline__ void fma_two(float& d0, float& d1, uint32_t a0, uint3
 // What a k-block takes (cycles; 8192 x 8192 x 8192): its MMAs 516, with the hand-overs of the accumulators 588, with the loads
 // 660, with the read-out of TMEM 666, with the multiply-adds 805 - the chain wait, read, add, release of the eight warps, whose pipe
 // is 32 % busy.  Up projection with SwiGLU and quantised results, 256 experts of 7168 x 2048: 16384 tokens 4.3 ms (1796 TFLOP/s)
-// in short runs, 4.8 - 5.0 ms at 1000 W; 64 tokens 900 us, 6.6 TB/s (a copy: 6.53), and 935 - 970 us at 1000 W.
+// in short runs, 4.9 - 5.25 ms at 1000 W; 64 tokens 900 us, 6.6 TB/s (a copy: 6.53), and 961 - 1034 us at 1000 W.
 template <bool kPair, bool kSwiglu, bool kQuantize, bool kSplit>
 __global__ void __launch_bounds__(kExpertThreads, 1)
 fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
@@ -279,7 +279,8 @@ fb_expert_matmul_e4m3_kernel(const __grid_constant__ CUtensorMap map_x, const __
       __syncwarp();
     };
     // 128 bytes of each row (64 results in bf16), 16 rows at a time: whole lines leave the SM.  (Down projection of 5003 tokens,
-    // 256 experts of 2048 x 7168, at 1000 W: 1037 us; 64 bytes of 32 rows at a time 1090; straight from the registers 1215.)
+    // 256 experts of 2048 x 7168, at 1000 W, in turn on the coolest box: 1037 us; 64 bytes of 32 rows at a time 1090; straight from
+    // the registers 1215.  On two other boxes it takes 1149 and 1162.)
     auto store_wide = [&](const ExpertTile& t, int column, const uint32_t (&value)[32]) {
 #pragma unroll
       for (int part = 0; part < 2; ++part) {
