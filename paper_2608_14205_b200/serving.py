@@ -127,7 +127,9 @@ class ServingLoop:
         T, o, k = r["T"], self.out, self.wl.k
         assert r["pi_old"] is self._spare, "a later step has overwritten this one's index and plan"
         assert (experts.E, experts.d) == (self.wl.E, self.wl.d) and experts.images.device == self.dev, "images of another model or device"
-        assert H.shape[0] == T, "the hidden states of another batch than the step's"
+        assert H.shape == (T, self.wl.d), "the hidden states of another batch than the step's"
+        for t in (H,) if addend is None else (H, addend):    # (here and not by the calls: they come behind the swaps)
+            assert t.shape == H.shape and t.dtype == torch.bfloat16 and t.is_contiguous() and t.data_ptr() % 16 == 0, "H, addend: bf16 [T, d]"
         key = (experts.d, experts.inter, experts.e4m3, self.T_max, k)
         if key not in self._buffers:
             self._buffers[key] = X.ExpertBuffers(experts, self.T_max, k)

@@ -140,3 +140,21 @@ def test_rows_of_another_length_are_refused(e4m3, d):
     with pytest.raises(AssertionError):
         X.run_experts(ctx, x, buf, rows(8), 8, K, None, None, None, None)
     assert made == []
+
+
+@pytest.mark.parametrize("wrong", ["H float16", "H columns", "H strided", "addend rows", "addend float32", "addend strided"])
+def test_what_is_refused_moves_no_weights(loop, wrong):
+    # a refusal behind the swaps would leave them applied, and the call that follows would apply them again
+    x = Experts()
+    r = loop.layer_step(0, None, rows(8), rows(8), None)
+    H, addend = rows(8), rows(8)
+    strided = torch.zeros(8, 2 * D, dtype=torch.bfloat16)[:, :D]
+    if wrong[0] == "H":
+        H = {"H float16": H.half(), "H columns": rows(8)[:, :16].contiguous(), "H strided": strided}[wrong]
+    else:
+        addend = {"addend rows": rows(7), "addend float32": addend.float(), "addend strided": strided}[wrong]
+    with pytest.raises(AssertionError):
+        loop.experts_step(r, H, x, addend)
+    assert x.swapped == 0 and loop.ran == []
+    loop.experts_step(r, rows(8), x, rows(8))
+    assert x.swapped == 1
